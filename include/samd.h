@@ -507,6 +507,81 @@ int samd_lanewise(int op, const uint32_t *a, const uint32_t *b, int64_t nwords, 
  * Arguments as samd_lanewise. */
 int samd_scale(const uint32_t *a, int64_t nwords, samd_fmt f, int32_t scalar, uint32_t *dst, hipStream_t stream);
 
+/* ---- Group-scaled rows: float tensors in 4 or 8 bits, and products with them ----
+ * The layers of a language model keep float activations and store their weights (and, for
+ * a backward pass, some activations) in few bits.  A group-scaled tensor of `rows` x
+ * `cols` values is
+ *   q      packed rows in the storage format above (samd_row_words(cols, f) words a row),
+ *          f.bits 4 or 8
+ *   scale  rows x groups float, groups = ceil(cols / group): consecutive values of a row
+ *          share a scale `group` at a time (32, 64 or 128; a row's last group may be
+ *          shorter)
+ *   zero   rows x groups uint8 whole zero points when f is unsigned, NULL when it is signed
+ * and stands for  value[r][j] = scale[r][j / group] * (q[r][j] - zero[r][j / group])
+ * (zero 0 when signed).  All three are dense.
+ *
+ * Float tensors are row-major with a row stride in elements (`ld...`, at least the row's
+ * length; what lies between a row's end and the next row is neither read nor written) and
+ * an element type.  They must be aligned to their element (SAMD_EALIGN); rows that all
+ * start on 16 bytes are read and written fastest.  Sums and scales are 32-bit floats
+ * whatever the type; a result is rounded once, to the type, unless a call says more.
+ * Sizes are at most 2^31 - 1 each, offsets are 64-bit.  Inputs and outputs must not
+ * overlap.  No call needs a workspace, and a call's results do not depend on what else
+ * runs: no atomics, a fixed order of every sum. */
+enum { SAMD_F32 = 0, SAMD_F16 = 1, SAMD_BF16 = 2 };
+
+/* src (rows x cols, row stride ld) to group-scaled rows.  In 32-bit floats, fl() a rounding
+ * to float and rint() one to the nearest whole number, halves to even:
+ *   signed    top = 2^(b-1) - 1, span = the group's largest |x|, zero = 0
+ *   unsigned  top = 2^b - 1, lo = min(0, least x), span = fl(max(0, largest x) - lo),
+ *             zero = clamp(rint(fl(-lo inv)), 0, top)
+ *   inv = fl(top / span), scale = fl(span fl(1 / top)),
+ *   q = clamp(rint(fl(x inv)) + zero, -top or 0, top)
+ * A group whose span is below 2^-100 gets scale, zero and q 0; one whose span is not
+ * finite (an infinity or a NaN among its values) gets scale NaN and zero and q 0, so that
+ * it is read back as NaN. */
+int samd_group_quantize(const void *src, int32_t type, int64_t rows, int64_t cols, int64_t ld, samd_fmt f,
+                        int32_t group, uint32_t *q, float *scale, uint8_t *zero, hipStream_t stream);
+
+/* Group-scaled rows to float rows: dst[r][j] = the value, rounded to the type. */
+int samd_group_dequantize(const uint32_t *q, const float *scale, const uint8_t *zero, int64_t rows, int64_t cols,
+                          samd_fmt f, int32_t group, void *dst, int32_t type, int64_t ld, hipStream_t stream);
+
+/* y = x W^T: x is T x K, W is M group-scaled rows of K 4-bit values (wf.bits 4), y is T x M
+ * of x's type.  T = 1 is a matrix-vector product.  An x row that holds an infinity or a NaN
+ * gives a y row of NaN and infinities. */
+int samd_group_matmul(const void *x, int32_t type, int64_t ldx, const uint32_t *q, const float *scale,
+                      const uint8_t *zero, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K, void *y,
+                      int64_t ldy, hipStream_t stream);
+
+/* dx = dy W, the gradient of samd_group_matmul with respect to x (W itself is frozen):
+ * dy is T x M, dx is T x K.  With dy2 and q2, scale2, zero2 given (all of them, zero2 when
+ * wf is unsigned), dx = dy W + dy2 W2, both sums before the one rounding: the input
+ * gradient of samd_group_gated.  dy and dy2 have the same row stride. */
+int samd_group_matmul_grad(const void *dy, int32_t type, int64_t lddy, const uint32_t *q, const float *scale,
+                           const uint8_t *zero, const void *dy2, const uint32_t *q2, const float *scale2,
+                           const uint8_t *zero2, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K,
+                           void *dx, int64_t lddx, hipStream_t stream);
+
+/* The gated half of a feed-forward block: g = x Wg^T, u = x Wu^T, h = act(g) u (T x M).
+ *   act  SAMD_ACT_SILU: g / (1 + e^-g);  SAMD_ACT_GELU: g (1 + erf(g / sqrt 2)) / 2
+ * g and u stay in 32-bit floats.  With g8, gscale, u8 and uscale given (all of them), g and
+ * u are also stored for the backward pass as samd_group_quantize would store them: signed
+ * 8-bit rows of M values with a scale for every SAMD_GATED_GROUP, 9 bits a value. */
+enum { SAMD_ACT_SILU = 0, SAMD_ACT_GELU = 1 };
+#define SAMD_GATED_GROUP 32
+int samd_group_gated(const void *x, int32_t type, int64_t ldx, const uint32_t *qg, const float *scaleg,
+                     const uint8_t *zerog, const uint32_t *qu, const float *scaleu, const uint8_t *zerou, samd_fmt wf,
+                     int32_t group, int32_t act, int64_t T, int64_t M, int64_t K, void *h, int64_t ldh, uint32_t *g8,
+                     float *gscale, uint32_t *u8, float *uscale, hipStream_t stream);
+
+/* The gradients of h = act(g) u from projections stored in 8 bits (signed group-scaled rows,
+ * T x M): dg = dh u act'(g), du = dh act(g), of dh's type.  dh has row stride lddh, dg and
+ * du ldd. */
+int samd_group_gated_grad(const void *dh, int32_t type, int64_t lddh, const uint32_t *g8, const float *gscale,
+                          const uint32_t *u8, const float *uscale, int32_t group, int32_t act, int64_t T, int64_t M,
+                          void *dg, void *du, int64_t ldd, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

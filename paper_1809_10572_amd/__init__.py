@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import List, Optional, Sequence, Tuple
+from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -25,6 +25,8 @@ __all__ = ["Fmt", "Conv2dDesc", "Conv1dPlan", "Conv2dPlan", "SamdError", "lib", 
            "conv2d_int8_candidates", "conv2d_int8_use_plan",
            "SpacedLayout", "conv2d_spaced_layout", "conv2d_spaced_plan", "conv2d_spaced_workspace", "conv2d_spaced_prepare",
            "conv2d_spaced_pack", "conv2d_spaced_from_packed", "conv2d_spaced", "relu_requant_spaced", "conv2d_spaced_tune", "max_i32",
+           "GroupRows", "group_quantize", "group_dequantize", "group_matmul", "group_matmul_grad", "group_gated",
+           "group_gated_save", "group_gated_grad",
            "relu_requant_pack", "relu_requant_nhwc_u8", "out_hw", "peak_launch", "peak_work", "LIB_PATH"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsamd.so")
@@ -169,6 +171,15 @@ def lib():
                                                                  ctypes.POINTER(_sz)]),
             "samd_conv2d_spaced_tune": (ctypes.c_int, [_p, Fmt, _p, Fmt, ctypes.POINTER(Conv2dDesc), _p, _p, _sz, _i32,
                                                        _i32, ctypes.POINTER(Conv2dPlan), _p]),
+            "samd_group_quantize": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, Fmt, _i32, _p, _p, _p, _p]),
+            "samd_group_dequantize": (ctypes.c_int, [_p, _p, _p, _i64, _i64, Fmt, _i32, _p, _i32, _i64, _p]),
+            "samd_group_matmul": (ctypes.c_int, [_p, _i32, _i64, _p, _p, _p, Fmt, _i32, _i64, _i64, _i64, _p, _i64, _p]),
+            "samd_group_matmul_grad": (ctypes.c_int, [_p, _i32, _i64, _p, _p, _p, _p, _p, _p, _p, Fmt, _i32, _i64, _i64,
+                                                      _i64, _p, _i64, _p]),
+            "samd_group_gated": (ctypes.c_int, [_p, _i32, _i64, _p, _p, _p, _p, _p, _p, Fmt, _i32, _i32, _i64, _i64, _i64,
+                                                _p, _i64, _p, _p, _p, _p, _p]),
+            "samd_group_gated_grad": (ctypes.c_int, [_p, _i32, _i64, _p, _p, _p, _p, _i32, _i32, _i64, _i64, _p, _p, _i64,
+                                                     _p]),
             "samd_peak_launch": (ctypes.c_int, [ctypes.c_int, _i64, _i32, _p, _p, _i64, _p]),
             "samd_peak_work": (ctypes.c_double, [ctypes.c_int, _i64, _i32, _i64]),
         }
@@ -761,3 +772,235 @@ def conv2d_spaced_tune(xp: torch.Tensor, xfmt: Fmt, wp: torch.Tensor, wfmt: Fmt,
                                          ws.data_ptr(), _ws_bytes(ws), candidates, reps, ctypes.byref(plan),
                                          _stream(xp)))
     return plan
+
+
+# --- group-scaled rows (include/samd.h, "Group-scaled rows") ------------------------------
+
+GATED_GROUP = 32
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_ACTS = {"silu": 0, "gelu": 1}
+_FMTS = {(b, s): Fmt(b, s) for b in range(1, 9) for s in (False, True)}
+
+
+class GroupRows(NamedTuple):
+    """Rows of `cols` values in 4 or 8 bits, scaled `group` at a time:
+    value = scale[..., j // group] * (q_j - zero[..., j // group]).
+
+    q      int32 words, (..., row_words(cols, bits))
+    scale  float32, (..., ceil(cols / group))
+    zero   uint8 zero points of scale's shape where the values are unsigned, else None"""
+    q: torch.Tensor
+    scale: torch.Tensor
+    zero: Optional[torch.Tensor]
+    cols: int
+    bits: int
+    group: int
+
+
+def _launch(fn, t: torch.Tensor, *args) -> None:
+    """Call an entry point on t's device and that device's current stream."""
+    at = t.get_device()
+    if at < 0 or at == torch.cuda.current_device():
+        status = fn(*args, _stream(t))
+    else:
+        with torch.cuda.device(at):
+            status = fn(*args, _stream(t))
+    if status != SAMD_OK:
+        _check(status)
+
+
+def _matrix(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> Tuple[int, int, int]:
+    """(rows, columns, row stride) of a float tensor: contiguous, its leading axes taken as
+    rows, or two-dimensional with contiguous rows.  `like`: of that tensor's type and device."""
+    if not isinstance(t, torch.Tensor) or not _on_gpu(t):
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
+        raise ValueError(f"{name} must have the type and device of the other operands")
+    if t.dim() == 0:
+        raise ValueError(f"{name} must have at least one axis")
+    cols = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // cols if cols else 0), cols, cols
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= cols:
+        return t.shape[0], cols, t.stride(0)
+    raise ValueError(f"{name} must be contiguous, or two-dimensional with contiguous rows")
+
+
+def _group_rows(r: GroupRows, name: str, like: torch.Tensor) -> int:
+    """Check a group-scaled tensor against its own sizes; returns its row count."""
+    q, scale, zero, cols, bits, group = r
+    if group not in (32, 64, 128) or bits not in (4, 8) or cols < 0:
+        raise ValueError(f"{name}: groups of 32, 64 or 128 values of 4 or 8 bits")
+    words, groups = -(-cols * bits // 32), -(-cols // group)
+    _dev(q, torch.int32, f"{name}.q")
+    _dev(scale, torch.float32, f"{name}.scale")
+    if q.dim() == 0 or q.shape[-1] != words:
+        raise ValueError(f"{name}.q must have rows of {words} words for {cols} values")
+    rows = q.numel() // words if words else 0
+    if scale.numel() != rows * groups:
+        raise ValueError(f"{name}.scale must hold {rows} x {groups} values")
+    if zero is not None:
+        _dev(zero, torch.uint8, f"{name}.zero")
+        if zero.numel() != rows * groups:
+            raise ValueError(f"{name}.zero must hold {rows} x {groups} values")
+    at = like.get_device()
+    if q.get_device() != at or scale.get_device() != at or (zero is not None and zero.get_device() != at):
+        raise ValueError(f"{name} must be on the device of the other operands")
+    return rows
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _out_matrix(out: Optional[torch.Tensor], shape, like: torch.Tensor, name: str = "out") -> Tuple[torch.Tensor, int]:
+    """The result tensor and its row stride."""
+    if out is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device), shape[-1]
+    rows, cols, ld = _matrix(out, name, like)
+    want = 1
+    for n in shape[:-1]:
+        want *= n
+    if cols != shape[-1] or (cols and rows != want):
+        raise ValueError(f"{name} must hold {want} rows of {shape[-1]} values")
+    return out, ld
+
+
+def _act_code(act: str) -> int:
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}, got {act!r}")
+    return _ACTS[act]
+
+
+def group_quantize(x: torch.Tensor, bits: int, signed: bool, group: int = 128) -> GroupRows:
+    """The last axis of a float tensor in 4 or 8 bits with a scale (and, unsigned, a zero
+    point) for every `group` values: weights once, activations kept for a backward pass."""
+    rows, cols, ld = _matrix(x, "x")
+    if group not in (32, 64, 128) or bits not in (4, 8):
+        raise ValueError("groups of 32, 64 or 128 values of 4 or 8 bits")
+    lead, shape = x.shape[:-1], x.shape[:-1] + (-(-cols // group),)
+    q = torch.empty(lead + (-(-cols * bits // 32),), dtype=torch.int32, device=x.device)
+    scale = torch.empty(shape, dtype=torch.float32, device=x.device)
+    zero = None if signed else torch.empty(shape, dtype=torch.uint8, device=x.device)
+    _launch(lib().samd_group_quantize, x, x.data_ptr(), _TYPES[x.dtype], rows, cols, ld, _FMTS[bits, bool(signed)], group,
+            q.data_ptr(), scale.data_ptr(), _ptr(zero))
+    return GroupRows(q, scale, zero, cols, bits, group)
+
+
+def group_dequantize(r: GroupRows, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of group-scaled rows, rounded to `dtype`."""
+    rows = _group_rows(r, "r", r.q)
+    if out is None:
+        if dtype not in _TYPES:
+            raise ValueError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+        out, ld = torch.empty(r.q.shape[:-1] + (r.cols,), dtype=dtype, device=r.q.device), r.cols
+    else:
+        orows, ocols, ld = _matrix(out, "out")
+        if ocols != r.cols or (r.cols and orows != rows) or out.get_device() != r.q.get_device():
+            raise ValueError(f"out must hold {rows} rows of {r.cols} values on the device of r")
+    _launch(lib().samd_group_dequantize, r.q, r.q.data_ptr(), r.scale.data_ptr(), _ptr(r.zero), rows, r.cols,
+            _FMTS[r.bits, r.zero is None], r.group, out.data_ptr(), _TYPES[out.dtype], ld)
+    return out
+
+
+def _weights(w: GroupRows, name: str, like: torch.Tensor, rows: Optional[int], cols: Optional[int]) -> int:
+    n = _group_rows(w, name, like)
+    if w.bits != 4:
+        raise ValueError(f"{name} must hold 4-bit weights")
+    if rows is not None and n != rows:
+        raise ValueError(f"{name} must have {rows} rows, got {n}")
+    if cols is not None and w.cols != cols:
+        raise ValueError(f"{name} must have rows of {cols} values, got {w.cols}")
+    return n
+
+
+def _same_kind(a: GroupRows, b: GroupRows) -> None:
+    if a.group != b.group or (a.zero is None) != (b.zero is None):
+        raise ValueError("both weights must have one group size and signedness")
+
+
+def group_matmul(x: torch.Tensor, w: GroupRows, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x W^T for x (..., K) and M 4-bit weight rows of K values; one token or many."""
+    T, K, ldx = _matrix(x, "x")
+    M = _weights(w, "w", x, None, K)
+    out, ldy = _out_matrix(out, x.shape[:-1] + (M,), x)
+    _launch(lib().samd_group_matmul, x, x.data_ptr(), _TYPES[x.dtype], ldx, w.q.data_ptr(), w.scale.data_ptr(), _ptr(w.zero),
+            _FMTS[4, w.zero is None], w.group, T, M, K, out.data_ptr(), ldy)
+    return out
+
+
+def group_matmul_grad(dy: torch.Tensor, w: GroupRows, dy2: Optional[torch.Tensor] = None, w2: Optional[GroupRows] = None,
+                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dy W (+ dy2 W2): the gradient of group_matmul (or, with both pairs, of group_gated's
+    two products) with respect to x."""
+    T, M, ld = _matrix(dy, "dy")
+    K = w.cols
+    _weights(w, "w", dy, M, None)
+    if (dy2 is None) != (w2 is None):
+        raise ValueError("dy2 and w2 go together")
+    if dy2 is not None:
+        if _matrix(dy2, "dy2", dy) != (T, M, ld):
+            raise ValueError("dy2 must have the sizes and row stride of dy")
+        _weights(w2, "w2", dy, M, K)
+        _same_kind(w, w2)
+    out, ldx = _out_matrix(out, dy.shape[:-1] + (K,), dy)
+    second = (None,) * 4 if w2 is None else (dy2.data_ptr(), w2.q.data_ptr(), w2.scale.data_ptr(), _ptr(w2.zero))
+    _launch(lib().samd_group_matmul_grad, dy, dy.data_ptr(), _TYPES[dy.dtype], ld, w.q.data_ptr(), w.scale.data_ptr(),
+            _ptr(w.zero), *second, _FMTS[4, w.zero is None], w.group, T, M, K, out.data_ptr(), ldx)
+    return out
+
+
+def _gated(x: torch.Tensor, wg: GroupRows, wu: GroupRows, act: str, out: Optional[torch.Tensor], save: bool):
+    code = _act_code(act)
+    T, K, ldx = _matrix(x, "x")
+    M = _weights(wg, "wg", x, None, K)
+    _weights(wu, "wu", x, M, K)
+    _same_kind(wg, wu)
+    lead = x.shape[:-1]
+    out, ldh = _out_matrix(out, lead + (M,), x)
+    g = u = None
+    stored = (None,) * 4
+    if save:
+        def rows():
+            return GroupRows(torch.empty(lead + (-(-M // 4),), dtype=torch.int32, device=x.device),
+                             torch.empty(lead + (-(-M // GATED_GROUP),), dtype=torch.float32, device=x.device), None, M, 8,
+                             GATED_GROUP)
+        g, u = rows(), rows()
+        stored = (g.q.data_ptr(), g.scale.data_ptr(), u.q.data_ptr(), u.scale.data_ptr())
+    _launch(lib().samd_group_gated, x, x.data_ptr(), _TYPES[x.dtype], ldx, wg.q.data_ptr(), wg.scale.data_ptr(),
+            _ptr(wg.zero), wu.q.data_ptr(), wu.scale.data_ptr(), _ptr(wu.zero), _FMTS[4, wg.zero is None], wg.group, code,
+            T, M, K, out.data_ptr(), ldh, *stored)
+    return out, g, u
+
+
+def group_gated(x: torch.Tensor, wg: GroupRows, wu: GroupRows, act: str = "silu",
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(x Wg^T) * (x Wu^T), the gated half of a feed-forward block (act "silu" or "gelu")."""
+    return _gated(x, wg, wu, act, out, False)[0]
+
+
+def group_gated_save(x: torch.Tensor, wg: GroupRows, wu: GroupRows, act: str = "silu",
+                     out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, GroupRows, GroupRows]:
+    """group_gated, and both products stored in 8 bits for group_gated_grad: (h, g, u)."""
+    return _gated(x, wg, wu, act, out, True)
+
+
+def group_gated_grad(dh: torch.Tensor, g: GroupRows, u: GroupRows, act: str = "silu",
+                     out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dg, du) of h = act(g) u from the products stored by group_gated_save; group_matmul_grad
+    takes both on to dx."""
+    code = _act_code(act)
+    T, M, ldh = _matrix(dh, "dh")
+    for r, name in ((g, "g"), (u, "u")):
+        n = _group_rows(r, name, dh)
+        if r.bits != 8 or r.zero is not None or r.cols != M or (M and n != T) or r.group != g.group:
+            raise ValueError(f"{name} must hold {T} signed 8-bit rows of {M} values")
+    dg, ldd = _out_matrix(None if out is None else out[0], dh.shape, dh, "dg")
+    du, ldu = _out_matrix(None if out is None else out[1], dh.shape, dh, "du")
+    if ldu != ldd:
+        raise ValueError("dg and du must have one row stride")
+    _launch(lib().samd_group_gated_grad, dh, dh.data_ptr(), _TYPES[dh.dtype], ldh, g.q.data_ptr(), g.scale.data_ptr(),
+            u.q.data_ptr(), u.scale.data_ptr(), g.group, code, T, M, dg.data_ptr(), du.data_ptr(), ldd)
+    return dg, du

@@ -930,3 +930,183 @@ int samd_conv2d_untune(const samd_conv2d_desc *d, samd_fmt xf, samd_fmt wf) {
 }
 
 }  // extern "C"
+
+// ---- group-scaled rows ----------------------------------------------------------------
+
+namespace {
+
+int64_t type_size(int32_t type) { return type == SAMD_F32 ? 4 : 2; }
+
+int check_type(int32_t type) {
+    if (type != SAMD_F32 && type != SAMD_F16 && type != SAMD_BF16)
+        return fail(SAMD_EINVAL, "type %d is not SAMD_F32, SAMD_F16 or SAMD_BF16", type);
+    return SAMD_OK;
+}
+
+int check_group(samd_fmt f, int32_t group, bool weights) {
+    int st = check_fmt(f, "fmt");
+    if (st) return st;
+    if (f.bits != 4 && (weights || f.bits != 8))
+        return fail(SAMD_EUNSUPPORTED, "group-scaled %s of %d bits", weights ? "weights" : "rows", f.bits);
+    if (group != 32 && group != 64 && group != 128)
+        return fail(SAMD_EUNSUPPORTED, "group = %d is not 32, 64 or 128", group);
+    return SAMD_OK;
+}
+
+int check_size(int64_t n, int64_t least, const char *name) {
+    if (n < least || n > INT32_MAX)
+        return fail(SAMD_EINVAL, "%s = %lld is outside %lld..2^31 - 1", name, (long long)n, (long long)least);
+    return SAMD_OK;
+}
+
+// A float matrix: pointer, alignment to its element, row stride.
+int check_matrix(const void *p, int32_t type, int64_t rows, int64_t cols, int64_t ld, const char *name) {
+    if (!p) return fail(SAMD_EINVAL, "%s must not be NULL", name);
+    if ((uintptr_t)p & (type_size(type) - 1)) return fail(SAMD_EALIGN, "%s is not aligned to its elements", name);
+    if (ld < cols) return fail(SAMD_EINVAL, "the row stride of %s, %lld, is below its %lld columns", name, (long long)ld,
+                               (long long)cols);
+    if (rows > 1 && ld > INT64_MAX / 8 / rows)
+        return fail(SAMD_EINVAL, "the row stride of %s, %lld, is too large", name, (long long)ld);
+    return SAMD_OK;
+}
+
+int check_rows(const GroupW &w, samd_fmt f, const char *name) {
+    if (!w.q || !w.scale) return fail(SAMD_EINVAL, "the words and scales of %s must not be NULL", name);
+    if (f.is_signed ? w.zero != nullptr : w.zero == nullptr)
+        return fail(SAMD_EINVAL, f.is_signed ? "%s is signed and takes no zero points" : "%s is unsigned and needs zero points",
+                    name);
+    if (!aligned4(w.q) || !aligned4(w.scale)) return fail(SAMD_EALIGN, "the words or scales of %s are not aligned", name);
+    return SAMD_OK;
+}
+
+int check_act(int32_t act) {
+    if (act != SAMD_ACT_SILU && act != SAMD_ACT_GELU)
+        return fail(SAMD_EINVAL, "act %d is not SAMD_ACT_SILU or SAMD_ACT_GELU", act);
+    return SAMD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int samd_group_quantize(const void *src, int32_t type, int64_t rows, int64_t cols, int64_t ld, samd_fmt f,
+                        int32_t group, uint32_t *q, float *scale, uint8_t *zero, hipStream_t stream) {
+    set_error("");
+    int st = check_type(type);
+    if (!st) st = check_group(f, group, false);
+    if (!st) st = check_size(rows, 0, "rows");
+    if (!st) st = check_size(cols, 0, "cols");
+    if (st) return st;
+    if (rows == 0 || cols == 0) return SAMD_OK;
+    st = check_matrix(src, type, rows, cols, ld, "src");
+    if (!st) st = check_rows({q, scale, zero}, f, "the result");
+    if (st) return st;
+    return launch_group_quantize(src, type, rows, cols, ld, f, group, q, scale, zero, stream);
+}
+
+int samd_group_dequantize(const uint32_t *q, const float *scale, const uint8_t *zero, int64_t rows, int64_t cols,
+                          samd_fmt f, int32_t group, void *dst, int32_t type, int64_t ld, hipStream_t stream) {
+    set_error("");
+    int st = check_type(type);
+    if (!st) st = check_group(f, group, false);
+    if (!st) st = check_size(rows, 0, "rows");
+    if (!st) st = check_size(cols, 0, "cols");
+    if (st) return st;
+    if (rows == 0 || cols == 0) return SAMD_OK;
+    st = check_matrix(dst, type, rows, cols, ld, "dst");
+    if (!st) st = check_rows({q, scale, zero}, f, "the rows");
+    if (st) return st;
+    return launch_group_dequantize({q, scale, zero}, rows, cols, f, group, dst, type, ld, stream);
+}
+
+int samd_group_matmul(const void *x, int32_t type, int64_t ldx, const uint32_t *q, const float *scale,
+                      const uint8_t *zero, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K, void *y,
+                      int64_t ldy, hipStream_t stream) {
+    set_error("");
+    int st = check_type(type);
+    if (!st) st = check_group(wf, group, true);
+    if (!st) st = check_size(T, 0, "T");
+    if (!st) st = check_size(M, 0, "M");
+    if (!st) st = check_size(K, 1, "K");
+    if (st) return st;
+    if (T == 0 || M == 0) return SAMD_OK;
+    st = check_matrix(x, type, T, K, ldx, "x");
+    if (!st) st = check_matrix(y, type, T, M, ldy, "y");
+    if (!st) st = check_rows({q, scale, zero}, wf, "the weights");
+    if (st) return st;
+    GroupProduct p{};
+    p.x = x, p.type = type, p.ldx = ldx, p.w[0] = {q, scale, zero}, p.group = group, p.act = -1;
+    p.T = (int32_t)T, p.M = (int32_t)M, p.K = (int32_t)K, p.y = y, p.ldy = ldy;
+    return launch_group_product(p, stream);
+}
+
+int samd_group_matmul_grad(const void *dy, int32_t type, int64_t lddy, const uint32_t *q, const float *scale,
+                           const uint8_t *zero, const void *dy2, const uint32_t *q2, const float *scale2,
+                           const uint8_t *zero2, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K,
+                           void *dx, int64_t lddx, hipStream_t stream) {
+    set_error("");
+    int st = check_type(type);
+    if (!st) st = check_group(wf, group, true);
+    if (!st) st = check_size(T, 0, "T");
+    if (!st) st = check_size(M, 1, "M");
+    if (!st) st = check_size(K, 0, "K");
+    if (st) return st;
+    if (T == 0 || K == 0) return SAMD_OK;
+    const bool two = dy2 || q2 || scale2 || zero2;
+    st = check_matrix(dy, type, T, M, lddy, "dy");
+    if (!st) st = check_matrix(dx, type, T, K, lddx, "dx");
+    if (!st) st = check_rows({q, scale, zero}, wf, "the weights");
+    if (!st && two) st = check_matrix(dy2, type, T, M, lddy, "dy2");
+    if (!st && two) st = check_rows({q2, scale2, zero2}, wf, "the second weights");
+    if (st) return st;
+    return launch_group_matmul_grad({{dy, dy2}, type, lddy, {{q, scale, zero}, {q2, scale2, zero2}}, group, (int32_t)T,
+                                     (int32_t)M, (int32_t)K, dx, lddx}, stream);
+}
+
+int samd_group_gated(const void *x, int32_t type, int64_t ldx, const uint32_t *qg, const float *scaleg,
+                     const uint8_t *zerog, const uint32_t *qu, const float *scaleu, const uint8_t *zerou, samd_fmt wf,
+                     int32_t group, int32_t act, int64_t T, int64_t M, int64_t K, void *h, int64_t ldh, uint32_t *g8,
+                     float *gscale, uint32_t *u8, float *uscale, hipStream_t stream) {
+    set_error("");
+    int st = check_type(type);
+    if (!st) st = check_group(wf, group, true);
+    if (!st) st = check_act(act);
+    if (!st) st = check_size(T, 0, "T");
+    if (!st) st = check_size(M, 0, "M");
+    if (!st) st = check_size(K, 1, "K");
+    if (st) return st;
+    if (T == 0 || M == 0) return SAMD_OK;
+    const bool save = g8 || gscale || u8 || uscale;
+    st = check_matrix(x, type, T, K, ldx, "x");
+    if (!st) st = check_matrix(h, type, T, M, ldh, "h");
+    if (!st) st = check_rows({qg, scaleg, zerog}, wf, "the gate's weights");
+    if (!st) st = check_rows({qu, scaleu, zerou}, wf, "the other weights");
+    if (!st && save) st = check_rows({g8, gscale, nullptr}, {8, 1}, "the stored gate");
+    if (!st && save) st = check_rows({u8, uscale, nullptr}, {8, 1}, "the other stored projection");
+    if (st) return st;
+    return launch_group_product({x, type, ldx, {{qg, scaleg, zerog}, {qu, scaleu, zerou}}, group, act, (int32_t)T,
+                                 (int32_t)M, (int32_t)K, h, ldh, g8, u8, gscale, uscale}, stream);
+}
+
+int samd_group_gated_grad(const void *dh, int32_t type, int64_t lddh, const uint32_t *g8, const float *gscale,
+                          const uint32_t *u8, const float *uscale, int32_t group, int32_t act, int64_t T, int64_t M,
+                          void *dg, void *du, int64_t ldd, hipStream_t stream) {
+    set_error("");
+    int st = check_type(type);
+    if (!st) st = check_group({8, 1}, group, false);
+    if (!st) st = check_act(act);
+    if (!st) st = check_size(T, 0, "T");
+    if (!st) st = check_size(M, 0, "M");
+    if (st) return st;
+    if (T == 0 || M == 0) return SAMD_OK;
+    st = check_matrix(dh, type, T, M, lddh, "dh");
+    if (!st) st = check_matrix(dg, type, T, M, ldd, "dg");
+    if (!st) st = check_matrix(du, type, T, M, ldd, "du");
+    if (!st) st = check_rows({g8, gscale, nullptr}, {8, 1}, "the stored gate");
+    if (!st) st = check_rows({u8, uscale, nullptr}, {8, 1}, "the other stored projection");
+    if (st) return st;
+    return launch_group_gated_grad(dh, type, lddh, {g8, gscale, nullptr}, {u8, uscale, nullptr}, group, act, T, M, dg,
+                                   du, ldd, stream);
+}
+
+}  // extern "C"

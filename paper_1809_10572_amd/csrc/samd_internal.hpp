@@ -186,6 +186,48 @@ int launch_relu_requant_stage(const int32_t *acc, const int32_t *dev_max, const 
 int launch_relu_requant_nhwc_u8(const int32_t *acc, int N, int C, int H, int W, const int32_t *dev_max,
                                 int bits, uint8_t *dst, hipStream_t s);
 
+// Group-scaled rows (arguments checked by the callers in api.cpp).
+struct GroupW {              // one group-scaled tensor
+    const uint32_t *q;
+    const float *scale;
+    const uint8_t *zero;     // NULL: signed
+};
+int launch_group_quantize(const void *src, int type, int64_t rows, int64_t cols, int64_t ld, samd_fmt f, int group,
+                          uint32_t *q, float *scale, uint8_t *zero, hipStream_t s);
+int launch_group_dequantize(const GroupW &w, int64_t rows, int64_t cols, samd_fmt f, int group, void *dst, int type,
+                            int64_t ld, hipStream_t s);
+int launch_group_gated_grad(const void *dh, int type, int64_t lddh, const GroupW &g, const GroupW &u, int group, int act,
+                            int64_t T, int64_t M, void *dg, void *du, int64_t ldd, hipStream_t s);
+
+// act -1: y = x W[0]^T; else h = act(x W[0]^T) * (x W[1]^T), with both products stored in 8 bits
+// where g8 is not NULL.
+struct GroupProduct {
+    const void *x;
+    int type;
+    int64_t ldx;
+    GroupW w[2];
+    int group, act;
+    int32_t T, M, K;
+    void *y;
+    int64_t ldy;
+    uint32_t *g8, *u8;
+    float *gscale, *uscale;
+};
+int launch_group_product(const GroupProduct &p, hipStream_t s);
+
+// dx = dy[0] W[0] (+ dy[1] W[1] where dy[1] is not NULL)
+struct GroupGrad {
+    const void *dy[2];
+    int type;
+    int64_t lddy;
+    GroupW w[2];
+    int group;
+    int32_t T, M, K;
+    void *dx;
+    int64_t lddx;
+};
+int launch_group_matmul_grad(const GroupGrad &p, hipStream_t s);
+
 // Error detail for the calling thread.
 void set_error(const std::string &msg);
 
