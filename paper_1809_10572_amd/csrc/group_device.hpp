@@ -61,6 +61,11 @@ __device__ __forceinline__ void store8(X *p, int n, bool vec, const float (&v)[8
     }
 }
 
+// A buffer descriptor of `bytes` bytes: reads behind them give 0.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(uint32_t)min(bytes, (int64_t)0xfffffffc), 0x00020000);
+}
+
 // Which row an item of a row-major range belongs to: a multiplication where all items are
 // below 2^31, a 64-bit division else.
 struct RowOf {

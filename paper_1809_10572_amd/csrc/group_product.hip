@@ -6,7 +6,7 @@
 // a word's sum of 8 products is scaled once, in 32-bit floats.
 #include <hip/hip_runtime.h>
 
-#include "group_device.hpp"
+#include "group_vector.hpp"
 
 namespace samd {
 
@@ -93,6 +93,19 @@ __global__ __launch_bounds__(256) void group_product_kernel(GroupProduct p, int 
 int launch_group_product(const GroupProduct &p, hipStream_t s) {
     const int words = (int)row_words(p.K, 4), groups = (p.K + p.group - 1) / p.group;
     const int gshift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
+    if (p.T <= 4 && !p.g8) {
+        with_type(p.type, [&](auto t) {
+            using X = decltype(t);
+            auto go = [&](auto is_signed) {
+                constexpr bool S = decltype(is_signed)::value;
+                if (p.act < 0) launch_vector<X, S, 1, -1>(p, words, groups, gshift, s);
+                else if (p.act == SAMD_ACT_SILU) launch_vector<X, S, 2, SAMD_ACT_SILU>(p, words, groups, gshift, s);
+                else launch_vector<X, S, 2, SAMD_ACT_GELU>(p, words, groups, gshift, s);
+            };
+            p.w[0].zero ? go(std::false_type{}) : go(std::true_type{});
+        });
+        return check_launch("group product");
+    }
     const int64_t blocks = (((int64_t)p.M + kRows - 1) / kRows) * (((int64_t)p.T + kTokens - 1) / kTokens);
     if (blocks > INT32_MAX) {
         set_error("group product: T x M needs too many workgroups");
