@@ -979,6 +979,13 @@ int check_rows(const GroupW &w, samd_fmt f, const char *name) {
     return SAMD_OK;
 }
 
+// Rows of weights: a row's length, where a kernel addresses some tens of rows by 32-bit offsets.
+int check_row_length(int64_t K) {
+    if (K > kMaxGroupCols)
+        return fail(SAMD_EUNSUPPORTED, "K = %lld: rows of more than 2^27 weights are not supported", (long long)K);
+    return SAMD_OK;
+}
+
 int check_act(int32_t act) {
     if (act != SAMD_ACT_SILU && act != SAMD_ACT_GELU)
         return fail(SAMD_EINVAL, "act %d is not SAMD_ACT_SILU or SAMD_ACT_GELU", act);
@@ -1028,6 +1035,7 @@ int samd_group_matmul(const void *x, int32_t type, int64_t ldx, const uint32_t *
     if (!st) st = check_size(T, 0, "T");
     if (!st) st = check_size(M, 0, "M");
     if (!st) st = check_size(K, 1, "K");
+    if (!st) st = check_row_length(K);
     if (st) return st;
     if (T == 0 || M == 0) return SAMD_OK;
     st = check_matrix(x, type, T, K, ldx, "x");
@@ -1050,6 +1058,7 @@ int samd_group_matmul_grad(const void *dy, int32_t type, int64_t lddy, const uin
     if (!st) st = check_size(T, 0, "T");
     if (!st) st = check_size(M, 1, "M");
     if (!st) st = check_size(K, 0, "K");
+    if (!st) st = check_row_length(K);
     if (st) return st;
     if (T == 0 || K == 0) return SAMD_OK;
     const bool two = dy2 || q2 || scale2 || zero2;
@@ -1074,6 +1083,7 @@ int samd_group_gated(const void *x, int32_t type, int64_t ldx, const uint32_t *q
     if (!st) st = check_size(T, 0, "T");
     if (!st) st = check_size(M, 0, "M");
     if (!st) st = check_size(K, 1, "K");
+    if (!st) st = check_row_length(K);
     if (st) return st;
     if (T == 0 || M == 0) return SAMD_OK;
     const bool save = g8 || gscale || u8 || uscale;

@@ -9,6 +9,9 @@ typedef _Float16 half_t;
 typedef __bf16 bf16_t;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef half_t half2_t __attribute__((ext_vector_type(2)));
+typedef bf16_t bf162_t __attribute__((ext_vector_type(2)));
 
 // Calls f(float{} / half_t{} / bf16_t{}) for an element type; the host has checked the type.
 template <class F>
@@ -61,9 +64,11 @@ __device__ __forceinline__ void store8(X *p, int n, bool vec, const float (&v)[8
     }
 }
 
-// A buffer descriptor of `bytes` bytes: reads behind them give 0.
+// A buffer descriptor of `bytes` bytes, filled up to a whole word (a word that holds the last value is
+// read whole, from within one page): reads of words behind them give 0.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(uint32_t)min(bytes, (int64_t)0xfffffffc), 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(uint32_t)min((bytes + 3) & ~(int64_t)3, (int64_t)0xfffffffc),
+                                             0x00020000);
 }
 
 // Which row an item of a row-major range belongs to: a multiplication where all items are
@@ -101,9 +106,8 @@ __device__ __forceinline__ GroupStep group_step(float span, uint32_t bits, float
 
 // The gated block's activation: a = act(g), da = act'(g).  With the 32-bit exponential and
 // error function, whose errors of a few units in the last place are far below the type's.
-template <int ACT>
-__device__ __forceinline__ void activation(float g, float &a, float &da) {
-    if constexpr (ACT == SAMD_ACT_SILU) {
+__device__ __forceinline__ void activation(int act, float g, float &a, float &da) {
+    if (act == SAMD_ACT_SILU) {
         const float p = 1.0f / (1.0f + expf(-g));
         a = g * p;
         da = p * (1.0f + g * (1.0f - p));
@@ -112,6 +116,84 @@ __device__ __forceinline__ void activation(float g, float &a, float &da) {
         a = g * p;
         da = p + g * expf(-0.5f * g * g) * 0.39894228040143268f;
     }
+}
+
+typedef half_t half8_t __attribute__((ext_vector_type(8)));
+typedef bf16_t bf168_t __attribute__((ext_vector_type(8)));
+
+// D = A B + C on 16 x 16 x 32; operands as four words of two 16-bit floats.
+template <class X>
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (std::is_same_v<X, half_t>)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf168_t, a), __builtin_bit_cast(bf168_t, b), c, 0, 0, 0);
+}
+
+// 16-bit pieces of 8 activations: the values themselves, or three bf16 pieces of 32-bit ones.
+template <class X>
+constexpr int kPieces = sizeof(X) == 4 ? 3 : 1;
+
+// 8 values of a row as they are stored.
+template <class X>
+struct Raw8 {
+    u32x4 v[sizeof(X) / 2];
+};
+
+template <class X>
+__device__ __forceinline__ Raw8<X> raw8(const X *p, int n) {   // any alignment, n of them in the row
+    X h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = i < n ? p[i] : (X)0.0f;
+    return __builtin_bit_cast(Raw8<X>, h);
+}
+
+// Zeroes behind the first n.
+template <class X>
+__device__ __forceinline__ void clear_behind(Raw8<X> &r, int n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(X) == 4) r.v[j / 4][j % 4] = j < n ? r.v[j / 4][j % 4] : 0u;
+        else r.v[0][j / 2] &= j < n ? 0xffffffffu : j % 2 ? 0x0000ffffu : 0u;
+    }
+}
+
+// The matrix operands of 8 values, in their order.  A 32-bit value goes into three bf16 pieces: its upper 8
+// significant bits, the next 8, the last 8, each by cutting the rest off, so that they add up to it.
+template <class X>
+__device__ __forceinline__ void x_operand(const Raw8<X> &raw, u32x4 (&out)[kPieces<X>]) {
+    if constexpr (sizeof(X) == 4) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(raw.v[i / 4][i % 4]);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)   // the upper halves of two values
+                out[j][i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] -= __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+        }
+    } else {
+        out[0] = raw.v[0];
+    }
+}
+
+// The same in the order in which pairs of fields come out of a word: 0, 4, 1, 5, 2, 6, 3, 7.
+template <class X>
+__device__ __forceinline__ void x_operand_paired(const Raw8<X> &raw, u32x4 (&out)[kPieces<X>]) {
+    x_operand(raw, out);
+#pragma unroll
+    for (int j = 0; j < kPieces<X>; ++j) {
+        const u32x4 w = out[j];
+        out[j] = u32x4{__builtin_amdgcn_perm(w[2], w[0], 0x05040100u), __builtin_amdgcn_perm(w[2], w[0], 0x07060302u),
+                       __builtin_amdgcn_perm(w[3], w[1], 0x05040100u), __builtin_amdgcn_perm(w[3], w[1], 0x07060302u)};
+    }
+}
+
+// Whether `rows` rows can be read through one buffer descriptor: on 4 bytes and within 4 GB.
+inline bool within_buffer(const void *p, int64_t size, int64_t rows, int64_t ld, int64_t cols) {
+    return ((uintptr_t)p & 3) == 0 && ld * size % 4 == 0 && ((__int128)rows * ld + cols) * size < (__int128)0xff000000;
 }
 
 }  // namespace samd

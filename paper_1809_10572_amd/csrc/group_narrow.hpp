@@ -1,0 +1,223 @@
+// Products of some tens of tokens with 4-bit group-scaled weights on the matrix cores.
+//
+// The weights still come from memory once, so they go straight into the registers that the
+// 16 x 16 x 32 matrix instruction reads: lane l holds row l % 16 of W, quarter l / 16 of the values that one
+// instruction sums over.  A step is 128 values of a row; which of them an instruction takes is free as long
+// as both operands agree and all lie in one group, so a lane's words are consecutive: PER = group / 32 words
+// for PER instructions.  As in the products of few tokens a field becomes the 16-bit float (16 + u) / 16
+// by half an operation, and an instruction on an operand of ones gives each token's sum of x:
+//   y += 16 s (sum x (16 + u)/16 - (1 + z/16) sum x)     once a group, in 32-bit floats.
+// 32-bit activations enter as three bf16 pieces of 8 bits each, which hold all 24 bits: the products stay
+// exact, three instructions for each.
+//
+// A workgroup computes 16 rows of W for 16 TT tokens, its eight waves taking steps of K in turn; their
+// sums meet in LDS in a fixed order.
+#pragma once
+
+#include "group_vector.hpp"
+
+namespace samd {
+
+constexpr int kNarrowWaves = 8;
+
+template <class X, bool SIGNED, int PER, int TT, int NW>
+__global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupProduct p, int words, int groups,
+                                                                         bool buffered) {
+    constexpr int kGroups = 4 / PER;   // groups of a step
+    constexpr int kTokens = 16 * TT, kRows = 16;
+    using H = std::conditional_t<std::is_same_v<X, half_t>, half_t, bf16_t>;
+    constexpr uint32_t kOnes = std::is_same_v<H, half_t> ? 0x3c003c00u : 0x3f803f80u;
+    constexpr uint32_t kField = std::is_same_v<H, half_t> ? (SIGNED ? 0x3e003e00u : 0x3c003c00u)
+                                                          : (SIGNED ? 0x3fc03fc0u : 0x3f803f80u);
+    constexpr int kPart = NW * TT * 4;   // sums of a lane
+    __shared__ float meet[kNarrowWaves * kPart * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int quarter = lane >> 4, low = lane & 15;
+    const int mblocks = (int)(((int64_t)p.M + kRows - 1) / kRows);
+    const int64_t m0 = (int64_t)(blockIdx.x % mblocks) * kRows, t0 = (int64_t)(blockIdx.x / mblocks) * kTokens;
+    const int rows = (int)min((int64_t)kRows, p.M - m0), tokens = (int)min((int64_t)kTokens, p.T - t0);
+    const int steps = (p.K + 127) / 128;
+
+    // Reads behind W's end give 0; what a row's last step reads of the next row meets an x of 0.
+    __amdgpu_buffer_rsrc_t rq[NW], rs[NW], rz[NW];
+#pragma unroll
+    for (int a = 0; a < NW; ++a) {
+        rq[a] = buffer_of(p.w[a].q + m0 * words, (int64_t)rows * words * 4);
+        rs[a] = buffer_of(p.w[a].scale + m0 * groups, (int64_t)rows * groups * 4);
+        rz[a] = buffer_of(p.w[a].zero + m0 * groups, SIGNED ? 0 : (int64_t)rows * groups);
+    }
+    const uint32_t qrow = (uint32_t)min(low, rows - 1) * (uint32_t)words, srow = (uint32_t)min(low, rows - 1) * (uint32_t)groups;
+    struct Step {
+        uint32_t w[NW][4];
+        float s[NW][kGroups];
+        uint32_t z[NW][kGroups];
+        Raw8<X> x[TT][4];
+    };
+    // the 8 values of a row of x that instruction i of a step takes in this lane
+    auto k_of = [&](int step, int i) { return step * 128 + (i / PER) * 32 * PER + quarter * 8 * PER + (i % PER) * 8; };
+
+    f32x4 acc[NW][TT] = {};
+    // BUF: rows of x on 4 bytes, within 4 GB of each other: read through one descriptor, any 4-byte alignment
+    auto body = [&](auto buf) {
+        constexpr bool BUF = decltype(buf)::value;
+        const __amdgpu_buffer_rsrc_t rx = buffer_of((const X *)p.x + t0 * p.ldx,
+                                                    ((int64_t)(tokens - 1) * p.ldx + p.K) * (int64_t)sizeof(X));
+        auto x_at = [&](int t, int step, int i) {
+            const int k = k_of(step, i), row = min(t * 16 + low, tokens - 1);
+            if constexpr (BUF) {
+                Raw8<X> r;
+                const uint32_t at = k < p.K && step < steps ? ((uint32_t)row * (uint32_t)p.ldx + k) * (uint32_t)sizeof(X) : 0xffffff00u;
+#pragma unroll
+                for (int c = 0; c < (int)sizeof(X) / 2; ++c) r.v[c] = __builtin_amdgcn_raw_buffer_load_b128(rx, at + 16 * c, 0, 0);
+                return r;
+            } else {
+                return raw8((const X *)p.x + (t0 + row) * p.ldx + k, step < steps ? p.K - k : 0);
+            }
+        };
+        auto fetch = [&](int step, Step &f) {
+#pragma unroll
+            for (int a = 0; a < NW; ++a) {
+#pragma unroll
+                for (int c = 0; c < kGroups; ++c) {
+                    const uint32_t at = step < steps ? (qrow + step * 16 + c * 4 * PER + quarter * PER) * 4 : 0xffffff00u;
+                    if constexpr (PER == 4) {
+                        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rq[a], at, 0, 0);
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) f.w[a][b] = v[b];
+                    } else if constexpr (PER == 2) {
+                        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rq[a], at, 0, 0);
+                        f.w[a][c * 2] = v[0], f.w[a][c * 2 + 1] = v[1];
+                    } else {
+                        f.w[a][c] = __builtin_amdgcn_raw_buffer_load_b32(rq[a], at, 0, 0);
+                    }
+                }
+                // a step's scales together; those behind the row's last group are not used below
+                const uint32_t g = srow + (uint32_t)min(step * kGroups, groups - 1);
+                if constexpr (kGroups == 4) {
+                    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs[a], g * 4, 0, 0);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) f.s[a][c] = __uint_as_float(v[c]);
+                } else if constexpr (kGroups == 2) {
+                    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs[a], g * 4, 0, 0);
+                    f.s[a][0] = __uint_as_float(v[0]), f.s[a][1] = __uint_as_float(v[1]);
+                } else {
+                    f.s[a][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs[a], g * 4, 0, 0));
+                }
+                if (!SIGNED)
+#pragma unroll
+                    for (int c = 0; c < kGroups; ++c) f.z[a][c] = __builtin_amdgcn_raw_buffer_load_b8(rz[a], g + c, 0, 0);
+            }
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f.x[t][i] = x_at(t, step, i);
+        };
+        auto use = [&](const Step &f, int step) {
+#pragma unroll
+            for (int c = 0; c < kGroups; ++c) {
+                f32x4 part[NW][TT] = {}, sum[TT] = {};
+#pragma unroll
+                for (int b = 0; b < PER; ++b) {
+                    const int i = c * PER + b;
+                    u32x4 x[TT][kPieces<X>];
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) {
+                        Raw8<X> r = f.x[t][i];
+                        if (BUF && step * 128 + 128 > p.K) clear_behind(r, p.K - k_of(step, i));
+                        x_operand_paired(r, x[t]);
+                    }
+                    const u32x4 ones = {kOnes, kOnes, kOnes, kOnes};
+#pragma unroll
+                    for (int t = 0; t < TT; ++t)
+#pragma unroll
+                        for (int j = 0; j < kPieces<X>; ++j) sum[t] = mfma<H>(x[t][j], ones, sum[t]);
+#pragma unroll
+                    for (int a = 0; a < NW; ++a) {
+                        const uint32_t w = f.w[a][i];
+                        const u32x4 v = {field_pair<H, 0>(w, kField), field_pair<H, 1>(w, kField), field_pair<H, 2>(w, kField),
+                                         field_pair<H, 3>(w, kField)};
+#pragma unroll
+                        for (int t = 0; t < TT; ++t)
+#pragma unroll
+                            for (int j = 0; j < kPieces<X>; ++j) part[a][t] = mfma<H>(x[t][j], v, part[a][t]);
+                    }
+                }
+                if (kGroups > 1 && step * kGroups + c >= groups) break;   // behind the row's last group
+#pragma unroll
+                for (int a = 0; a < NW; ++a) {
+                    const float z = SIGNED ? 8.0f : (float)f.z[a][c];
+                    const float zz = fmaf(z, -0.0625f, -1.0f), s = 16.0f * f.s[a][c];
+#pragma unroll
+                    for (int t = 0; t < TT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            acc[a][t][r] = fmaf(s, fmaf(zz, sum[t][r], part[a][t][r]), acc[a][t][r]);
+                }
+            }
+        };
+        Step f0, f1;
+        fetch(wave, f0);
+        int step = wave;
+        for (; step + kNarrowWaves < steps; step += 2 * kNarrowWaves) {
+            fetch(step + kNarrowWaves, f1);
+            use(f0, step);
+            fetch(step + 2 * kNarrowWaves, f0);
+            use(f1, step + kNarrowWaves);
+        }
+        if (step < steps) use(f0, step);
+    };
+    if (buffered) body(std::true_type{});
+    else body(std::false_type{});
+
+    // the waves' sums meet in LDS and are added in the waves' order
+#pragma unroll
+    for (int a = 0; a < NW; ++a)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) meet[(wave * kPart + (a * TT + t) * 4 + r) * 64 + lane] = acc[a][t][r];
+    __syncthreads();
+    for (int n = threadIdx.x; n < kTokens * kRows; n += 64 * kNarrowWaves) {
+        const int t = n / kRows, m = n % kRows;
+        if (t >= tokens || m >= rows) continue;
+        // lane (quarter, low) held tokens 4 quarter + r of row `low`
+        const int at = (t / 16 * 4 + t % 4) * 64 + t % 16 / 4 * 16 + m;
+        float v[NW] = {};
+#pragma unroll
+        for (int a = 0; a < NW; ++a)
+#pragma unroll
+            for (int w = 0; w < kNarrowWaves; ++w) v[a] += meet[(w * kPart + a * TT * 4) * 64 + at];
+        float out = v[0];
+        if constexpr (NW > 1) {
+            float da;
+            activation(p.act, v[0], out, da);
+            out *= v[1];
+        }
+        ((X *)p.y)[(t0 + t) * p.ldy + m0 + m] = (X)out;
+    }
+}
+
+// Launches the kernel: 16 tokens a workgroup, or 32.
+template <class X, bool SIGNED, int NW>
+int launch_narrow(const GroupProduct &p, int words, int groups, hipStream_t s) {
+    const int tt = p.T <= 16 ? 1 : 2;
+    const int64_t blocks = (((int64_t)p.M + 15) / 16) * (((int64_t)p.T + 16 * tt - 1) / (16 * tt));
+    if (blocks > INT32_MAX) {
+        set_error("group product: T x M needs too many workgroups");
+        return SAMD_EUNSUPPORTED;
+    }
+    const bool buffered = within_buffer(p.x, sizeof(X), std::min<int64_t>(p.T, 32), p.ldx, p.K);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * kNarrowWaves), 0, s, p, words, groups, buffered);
+    };
+    auto with_group = [&](auto per) {
+        constexpr int PER = decltype(per)::value;
+        tt == 1 ? go(group_narrow_kernel<X, SIGNED, PER, 1, NW>) : go(group_narrow_kernel<X, SIGNED, PER, 2, NW>);
+    };
+    if (p.group == 32) with_group(std::integral_constant<int, 1>{});
+    else if (p.group == 64) with_group(std::integral_constant<int, 2>{});
+    else with_group(std::integral_constant<int, 4>{});
+    return check_launch("group product");
+}
+
+}  // namespace samd

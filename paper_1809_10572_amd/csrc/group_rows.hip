@@ -129,12 +129,12 @@ __global__ __launch_bounds__(kBlock) void group_dequantize_kernel(const uint32_t
     }
 }
 
-template <class X, int ACT>
+template <class X>
 __global__ __launch_bounds__(kBlock) void group_gated_grad_kernel(const X *__restrict__ dh, int64_t lddh, GroupW g,
                                                                   GroupW u, int64_t items, int32_t M, int words,
                                                                   int groups, int gshift, RowOf div,
                                                                   X *__restrict__ dg, X *__restrict__ du, int64_t ldd,
-                                                                  bool vech, bool vecd, bool vecq) {
+                                                                  int act, bool vech, bool vecd, bool vecq) {
     for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < items; i += (int64_t)gridDim.x * kBlock) {
         const int64_t r = row_index(div, i);
         const int64_t at = i - r * div.per, k0 = at * 8;
@@ -148,10 +148,10 @@ __global__ __launch_bounds__(kBlock) void group_gated_grad_kernel(const X *__res
         load8(dh + r * lddh + k0, n, vech, d);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float act, slope;
-            activation<ACT>(sg * field_value<8, true>(fg[j], 0), act, slope);
+            float value, slope;
+            activation(act, sg * field_value<8, true>(fg[j], 0), value, slope);
             a[j] = d[j] * (su * field_value<8, true>(fu[j], 0)) * slope;
-            b[j] = d[j] * act;
+            b[j] = d[j] * value;
         }
         store8(dg + r * ldd + k0, n, vecd, a);
         store8(du + r * ldd + k0, n, vecd, b);
@@ -216,12 +216,9 @@ int launch_group_gated_grad(const void *dh, int type, int64_t lddh, const GroupW
     const bool vecq = words % 2 == 0 && (((uintptr_t)g.q | (uintptr_t)u.q) & 7) == 0;
     with_type(type, [&](auto t) {
         using X = decltype(t);
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), 0, s, (const X *)dh, lddh, g, u, items, (int32_t)M,
-                               words, (int)groups, group_shift(group), div, (X *)dg, (X *)du, ldd, vech, vecd, vecq);
-        };
-        act == SAMD_ACT_SILU ? go(group_gated_grad_kernel<X, SAMD_ACT_SILU>)
-                             : go(group_gated_grad_kernel<X, SAMD_ACT_GELU>);
+        hipLaunchKernelGGL((group_gated_grad_kernel<X>), dim3(grid), dim3(kBlock), 0, s, (const X *)dh, lddh, g, u, items,
+                           (int32_t)M, words, (int)groups, group_shift(group), div, (X *)dg, (X *)du, ldd, act, vech, vecd,
+                           vecq);
     });
     return check_launch("samd_group_gated_grad");
 }

@@ -28,10 +28,6 @@ constexpr int kVecWaves = 4;          // waves of a workgroup
 constexpr int kVecStep = 2048;        // values of a row per step: 64 lanes x 32
 constexpr int kVecLds = 32768;        // bytes of x held at once
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef half_t half2_t __attribute__((ext_vector_type(2)));
-typedef bf16_t bf162_t __attribute__((ext_vector_type(2)));
-
 // v of the lane that a data-parallel control names, within rows of 16 lanes.
 template <int CTRL>
 __device__ __forceinline__ float lane_swap(float v) {
@@ -70,7 +66,7 @@ __device__ __forceinline__ uint32_t field_pair(uint32_t w, uint32_t one) {
     return (t & (0x000f000fu << kAt)) ^ one;
 }
 
-template <class X, bool SIGNED, int T, int NW, int R, int ACT>
+template <class X, bool SIGNED, int T, int NW, int R>
 __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProduct p, int words, int groups, int gshift,
                                                                       int steps, int held, bool vecx) {
     constexpr bool kWide = sizeof(X) == 4;
@@ -207,9 +203,9 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
 #pragma unroll
         for (int t = 0; t < T; ++t) {
             float out = wave_sum(acc[0][r][t]);
-            if constexpr (ACT >= 0) {
+            if constexpr (NW > 1) {
                 float a, da;
-                activation<ACT>(out, a, da);
+                activation(p.act, out, a, da);
                 out = a * wave_sum(acc[NW - 1][r][t]);
             }
             if (lane == 0 && m0 + r < p.M && t < p.T) ((X *)p.y)[(int64_t)t * p.ldy + m0 + r] = (X)out;
@@ -219,7 +215,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
 // Launches the kernel for p.T tokens (at most 4).  Two rows a wave, so that x is read from LDS half as
 // often, unless that leaves CUs without a workgroup (1024 x 16384 weights: 7.4 us with one row a wave,
 // 9.5 with two; 16384 x 8192: 17.7 and 14.8).
-template <class X, bool SIGNED, int NW, int ACT>
+template <class X, bool SIGNED, int NW>
 void launch_vector(const GroupProduct &p, int words, int groups, int gshift, hipStream_t s) {
     const int steps = (words + 255) / 256;
     const bool vecx = rows16(p.x, p.type, p.ldx);
@@ -232,9 +228,9 @@ void launch_vector(const GroupProduct &p, int words, int groups, int gshift, hip
         hipLaunchKernelGGL(kernel, grid, dim3(64 * kVecWaves), held * step_bytes, s, p, words, groups, gshift, steps, held,
                            vecx);
     };
-    if (p.T == 1) one ? go(group_vector_kernel<X, SIGNED, 1, NW, 1, ACT>, 1) : go(group_vector_kernel<X, SIGNED, 1, NW, 2, ACT>, 1);
-    else if (p.T == 2) one ? go(group_vector_kernel<X, SIGNED, 2, NW, 1, ACT>, 2) : go(group_vector_kernel<X, SIGNED, 2, NW, 2, ACT>, 2);
-    else one ? go(group_vector_kernel<X, SIGNED, 4, NW, 1, ACT>, 4) : go(group_vector_kernel<X, SIGNED, 4, NW, 2, ACT>, 4);
+    if (p.T == 1) one ? go(group_vector_kernel<X, SIGNED, 1, NW, 1>, 1) : go(group_vector_kernel<X, SIGNED, 1, NW, 2>, 1);
+    else if (p.T == 2) one ? go(group_vector_kernel<X, SIGNED, 2, NW, 1>, 2) : go(group_vector_kernel<X, SIGNED, 2, NW, 2>, 2);
+    else one ? go(group_vector_kernel<X, SIGNED, 4, NW, 1>, 4) : go(group_vector_kernel<X, SIGNED, 4, NW, 2>, 4);
 }
 
 }  // namespace samd

@@ -187,6 +187,7 @@ int launch_relu_requant_nhwc_u8(const int32_t *acc, int N, int C, int H, int W, 
                                 int bits, uint8_t *dst, hipStream_t s);
 
 // Group-scaled rows (arguments checked by the callers in api.cpp).
+constexpr int64_t kMaxGroupCols = (int64_t)1 << 27;   // longest row of weights in a product
 struct GroupW {              // one group-scaled tensor
     const uint32_t *q;
     const float *scale;
@@ -213,7 +214,14 @@ struct GroupProduct {
     uint32_t *g8, *u8;
     float *gscale, *uscale;
 };
-int launch_group_product(const GroupProduct &p, hipStream_t s);
+int launch_group_product_f32(const GroupProduct &p, hipStream_t s);
+int launch_group_product_f16(const GroupProduct &p, hipStream_t s);
+int launch_group_product_bf16(const GroupProduct &p, hipStream_t s);
+inline int launch_group_product(const GroupProduct &p, hipStream_t s) {
+    return p.type == SAMD_F32   ? launch_group_product_f32(p, s)
+           : p.type == SAMD_F16 ? launch_group_product_f16(p, s)
+                                : launch_group_product_bf16(p, s);
+}
 
 // dx = dy[0] W[0] (+ dy[1] W[1] where dy[1] is not NULL)
 struct GroupGrad {

@@ -62,7 +62,8 @@ def close(got, want, bound, what=""):
     got = f64(got)
     assert got.shape == want.shape
     off = np.abs(got - want) - bound
-    assert np.isfinite(got).all() and (off <= 0).all(), (what, float(off.max()), np.unravel_index(off.argmax(), off.shape))
+    fine = bool(np.isfinite(got).all() and (off <= 0).all())
+    assert fine, (what, float(off.max()), np.unravel_index(off.argmax(), off.shape))
 
 
 def depth(n):
