@@ -982,7 +982,7 @@ int check_rows(const GroupW &w, samd_fmt f, const char *name) {
 // Rows of weights: a row's length, where a kernel addresses some tens of rows by 32-bit offsets.
 int check_row_length(int64_t K) {
     if (K > kMaxGroupCols)
-        return fail(SAMD_EUNSUPPORTED, "K = %lld: rows of more than 2^27 weights are not supported", (long long)K);
+        return fail(SAMD_EUNSUPPORTED, "K = %lld: rows of more than 2^25 weights are not supported", (long long)K);
     return SAMD_OK;
 }
 

@@ -191,6 +191,13 @@ __device__ __forceinline__ void x_operand_paired(const Raw8<X> &raw, u32x4 (&out
     }
 }
 
+// v, of which the compiler knows nothing: bytes of a masked word are converted to floats where they stand,
+// not cut out first.
+__device__ __forceinline__ uint32_t as_is(uint32_t v) {
+    asm("" : "+v"(v));
+    return v;
+}
+
 // Whether `rows` rows can be read through one buffer descriptor: on 4 bytes and within 4 GB.
 inline bool within_buffer(const void *p, int64_t size, int64_t rows, int64_t ld, int64_t cols) {
     return ((uintptr_t)p & 3) == 0 && ld * size % 4 == 0 && ((__int128)rows * ld + cols) * size < (__int128)0xff000000;

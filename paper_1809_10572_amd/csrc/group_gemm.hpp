@@ -4,7 +4,8 @@
 // exactly and scaled once for each group and output, in 32-bit floats: no weight is ever rounded.  32-bit
 // activations enter as three bf16 pieces (three instructions a product).
 //
-// A workgroup of TW x MW waves computes 16 WT TW tokens x 16 WM MW rows of W, a wave 16 WT x 16 WM.  Steps of 64
+// A workgroup computes 16 WT TW tokens x 16 WM MW rows of W with TW x MW waves for each of KS slices of K, a
+// wave 16 WT x 16 WM: large tiles where there are many tokens, slices where there are too few to fill the card.  Steps of 64
 // values: x (copied) and the fields (decoded once for the workgroup) go through LDS, two buffers, the next
 // step's loads in flight during this step's products.  A row of a buffer is 128 bytes, its 16-byte parts exchanged
 // by (row / 2) % 8, so that the 16 rows which an operand's lanes read meet no bank twice.
@@ -16,8 +17,10 @@
 
 namespace samd {
 
-constexpr int kGemmStep = 64;
+// A lambda that is part of its kernel however often it is called: its arrays have to stay in registers.
+#define SAMD_INLINE __attribute__((always_inline))
 
+constexpr int kGemmStep = 64;
 // Index of 16-byte part `c` (0..7) of row `r` in a buffer.
 __device__ __forceinline__ int part_at(int r, int c) { return r * 8 + (c ^ ((r >> 1) & 7)); }
 
@@ -35,7 +38,7 @@ __device__ __forceinline__ u32x4 whole_values(uint32_t w, int z) {
         return u32x4{__builtin_amdgcn_perm(t[1], t[0], 0x05040100u), __builtin_amdgcn_perm(t[3], t[2], 0x05040100u),
                      __builtin_amdgcn_perm(t[1], t[0], 0x07060302u), __builtin_amdgcn_perm(t[3], t[2], 0x07060302u)};
     } else {
-        const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
+        const uint32_t lo = as_is(w & 0x0f0f0f0fu), hi = as_is((w >> 4) & 0x0f0f0f0fu);
         const float zf = (float)z;
         u32x4 out;
 #pragma unroll
@@ -56,34 +59,35 @@ __device__ __forceinline__ uint32_t tile_of(uint32_t b, uint32_t n) {
 
 // Rows of a float matrix (from row r0 on, `rows` of them in range) on their way into LDS as matrix operands:
 // ROWS x 64 values a step.
-template <class X, int ROWS, int THREADS>
+// BUF: the rows are on 4 bytes and within 4 GB, and are read through one descriptor; else value by value.
+template <class X, int ROWS, int THREADS, bool BUF>
 struct TokenTile {
     static constexpr int kEach = ROWS * 8 / THREADS;   // 8-value parts of a thread
     Raw8<X> raw[kEach];
 
-    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t &rx, const X *x, int64_t ld, int rows, int cols, int step,
-                                         bool buffered) {
+    // What stands behind a row's end comes along and is cleared by store().
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t &rx, const X *x, int64_t ld, int rows, int cols, int step, int tid) {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int id = e * THREADS + threadIdx.x, k = step * kGemmStep + id % 8 * 8, row = min(id / 8, rows - 1);
-            if (buffered) {
-                const uint32_t at = k < cols ? ((uint32_t)row * (uint32_t)ld + k) * (uint32_t)sizeof(X) : 0xffffff00u;
+            const int row = min(e * (THREADS / 8) + tid / 8, rows - 1), k = tid % 8 * 8;
+            if constexpr (BUF) {
+                const uint32_t at = ((uint32_t)row * (uint32_t)ld + k) * (uint32_t)sizeof(X) + step * (kGemmStep * (int)sizeof(X));
 #pragma unroll
                 for (int c = 0; c < (int)sizeof(X) / 2; ++c)
                     raw[e].v[c] = __builtin_amdgcn_raw_buffer_load_b128(rx, at + 16 * c, 0, 0);
             } else {
-                raw[e] = raw8(x + row * ld + k, cols - k);
+                raw[e] = raw8(x + row * ld + step * kGemmStep + k, cols - step * kGemmStep - k);
             }
         }
     }
 
-    template <int P>
-    __device__ __forceinline__ void store(u32x4 (&to)[P][ROWS * 8], int cols, int step) {
-        const bool ragged = step * kGemmStep + kGemmStep > cols;
+    // RAGGED: the step may reach behind the rows' end.
+    template <bool RAGGED, int P>
+    __device__ __forceinline__ void store(u32x4 (&to)[P][ROWS * 8], int cols, int step, int tid) {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int id = e * THREADS + threadIdx.x;
-            if (ragged) clear_behind(raw[e], cols - (step * kGemmStep + id % 8 * 8));
+            const int id = e * THREADS + tid;
+            if (RAGGED) clear_behind(raw[e], cols - (step * kGemmStep + id % 8 * 8));
             u32x4 piece[P];
             x_operand(raw[e], piece);
 #pragma unroll
@@ -114,9 +118,9 @@ inline bool rows4(const void *p, int type, int64_t ld) {
     return (uintptr_t)p % bytes == 0 && ld % 4 == 0;
 }
 
-template <class X, int PER, int NW, int WT, int WM, int TW, int MW>
-__global__ __launch_bounds__(64 * TW * MW) void group_gemm_kernel(GroupProduct p, int words, int groups, int tblocks,
-                                                                  bool buffered, bool vecy) {
+template <class X, bool BUF, int PER, int NW, int WT, int WM, int TW, int MW, int KS>
+__global__ __launch_bounds__(64 * TW * MW * KS) void group_gemm_kernel(GroupProduct p, int words, int groups, int tblocks,
+                                                                  bool vecy) {
     using H = std::conditional_t<std::is_same_v<X, half_t>, half_t, bf16_t>;
     constexpr int P = kPieces<X>, THREADS = 64 * TW * MW;
     constexpr int BT = 16 * WT * TW, BM = 16 * WM * MW;      // tokens and rows of W of a workgroup
@@ -125,9 +129,17 @@ __global__ __launch_bounds__(64 * TW * MW) void group_gemm_kernel(GroupProduct p
     constexpr int TPR = 8 / WPT;                              // threads of a row
     constexpr int SG = PER == 1 ? 2 : 1;                      // groups of a step
     static_assert(64 / TPR <= 16 * WM / NW || NW == 1, "a wave decodes rows of one matrix");
-    __shared__ u32x4 xs[2][P][BT * 8], ws[2][BM * 8];
-    __shared__ float ss[2][SG * BM];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    struct Buffers {   // of one slice of K
+        u32x4 x[2][P][BT * 8], w[2][BM * 8];
+        float s[2][SG * BM];
+    };
+    static_assert((KS - 1) * BT * BM * 4 <= (int)sizeof(Buffers) * KS, "the slices' sums meet in the buffers");
+    __shared__ Buffers all[KS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % (TW * MW);
+    const int slice = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / (TW * MW), tid = threadIdx.x - slice * THREADS;
+    auto &xs = all[slice].x;
+    auto &ws = all[slice].w;
+    auto &ss = all[slice].s;
     const int quarter = lane >> 4, low = lane & 15, tw = wave % TW, mw = wave / TW;
     const uint32_t tile = tile_of(blockIdx.x, gridDim.x);
     const int64_t t0 = (int64_t)(tile % tblocks) * BT, m0 = (int64_t)(tile / tblocks) * OM;
@@ -139,101 +151,167 @@ __global__ __launch_bounds__(64 * TW * MW) void group_gemm_kernel(GroupProduct p
     // Row r of the buffer: a wave's 16 WM rows are first its rows of W[0], then those of W[1].  A wave decodes rows of one.
     auto matrix_of = [](int r) { return NW == 1 ? 0 : r % (16 * WM) / (8 * WM); };
     auto result_row = [](int r) { return NW == 1 ? r : r / (16 * WM) * (8 * WM) + r % (8 * WM); };
-    const int wrow = threadIdx.x / TPR, part = threadIdx.x % TPR * WPT;
+    const int wrow = tid / TPR, part = tid % TPR * WPT;
     const int a = __builtin_amdgcn_readfirstlane(matrix_of(wrow));
     const int row = result_row(wrow);
     const bool has_zero = p.w[0].zero != nullptr;
+    const uint32_t flip = has_zero ? 0u : 0x88888888u;
     const __amdgpu_buffer_rsrc_t rq = buffer_of(p.w[a].q + m0 * words, (int64_t)rows * words * 4);
     const __amdgpu_buffer_rsrc_t rz = buffer_of(p.w[a].zero + m0 * groups, has_zero ? (int64_t)rows * groups : 0);
     const uint32_t qrow = (uint32_t)row * (uint32_t)words, zrow = (uint32_t)row * (uint32_t)groups;
-    // scales: thread i loads that of row i of the buffer
-    static_assert(BM <= THREADS, "a thread loads the scales of one row");
-    const int srow = result_row(threadIdx.x % BM);
-    const bool scales = threadIdx.x < BM && srow < rows;
-    const float *const sp = p.w[matrix_of(threadIdx.x % BM)].scale + (m0 + (scales ? srow : 0)) * groups;
+    // scales: a thread loads those of row tid % BM of the buffer
+    static_assert(THREADS % BM == 0, "a thread loads the scales of one row");
+    const int srow = result_row(tid % BM);
+    const bool scales = srow < rows;
+    const float *const sp = p.w[matrix_of(tid % BM)].scale + (m0 + (scales ? srow : 0)) * groups;
 
-    TokenTile<X, BT, THREADS> xt;
-    uint32_t q[WPT];
-    int z;
-    float s[SG];
-    auto load = [&](int step) {
-        xt.load(rx, x, p.ldx, tokens, p.K, step, buffered);
-        const uint32_t at = step < steps && row < rows ? (qrow + step * 8 + part) * 4 : 0xffffff00u;
+    struct Step {
+        TokenTile<X, BT, THREADS, BUF> x;
+        uint32_t q[WPT], z;
+        float s[SG];
+    };
+    auto load = [&](Step &f, int step) SAMD_INLINE {
+        step = __builtin_amdgcn_readfirstlane(step);
+        asm("" : "+s"(step));   // addresses from one scalar each turn, not a register carried for each of them
+        f.x.load(rx, x, p.ldx, tokens, p.K, step, tid);
+        // steps behind the last get the next row's words, or zeros, for an x of zeros
+        const uint32_t at = (row < rows ? (qrow + part) * 4 : 0xc0000000u) + step * 32;
         if constexpr (WPT == 4) {
             const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rq, at, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = v[i];
+            for (int i = 0; i < 4; ++i) f.q[i] = v[i];
         } else {
             const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rq, at, 0, 0);
-            q[0] = v[0], q[1] = v[1];
+            f.q[0] = v[0], f.q[1] = v[1];
         }
         // a thread's words lie in one group
-        const uint32_t g = (uint32_t)((step * kGemmStep + part * 8) / (32 * PER));
-        z = has_zero ? (int)__builtin_amdgcn_raw_buffer_load_b8(rz, g < (uint32_t)groups ? zrow + g : 0xffffff00u, 0, 0) : 8;
+        f.z = __builtin_amdgcn_raw_buffer_load_b8(rz, zrow + (PER == 1 ? part / 4 : 0) + step * kGemmStep / (32 * PER), 0, 0);
 #pragma unroll
-        for (int c = 0; c < SG; ++c) {
-            const int gs = step * kGemmStep / (32 * PER) + c;
-            s[c] = scales && gs < groups ? sp[gs] : 0.0f;
-        }
+        for (int c = 0; c < SG; ++c) f.s[c] = sp[min(step * kGemmStep / (32 * PER) + c, groups - 1)];
     };
-    auto store = [&](int step, int buf) {
-        xt.store(xs[buf], p.K, step);
+    auto store = [&](auto ragged, Step &f, int step, int buf) SAMD_INLINE {
+        f.x.template store<decltype(ragged)::value>(xs[buf], p.K, step, tid);
 #pragma unroll
         for (int i = 0; i < WPT; ++i)
-            ws[buf][part_at(wrow, part + i)] = whole_values<H>(has_zero ? q[i] : q[i] ^ 0x88888888u, z);
-        if (threadIdx.x < BM)
+            ws[buf][part_at(wrow, part + i)] = whole_values<H>(f.q[i] ^ flip, has_zero ? (int)f.z : 8);
 #pragma unroll
-            for (int c = 0; c < SG; ++c) ss[buf][c * BM + threadIdx.x] = s[c];
+        for (int c = 0; c < SG; ++c)   // threads of one row write one value
+            ss[buf][c * BM + tid % BM] = scales && step * kGemmStep / (32 * PER) + c < groups ? f.s[c] : 0.0f;
     };
 
-    f32x4 acc[WM][WT] = {}, sum[WM][WT] = {};
-    auto flush = [&](int buf, int c) {
+    const int at[2] = {part_at(low, quarter), part_at(low, 4 + quarter)};   // the same in every 16 rows
+    f32x4 acc[WM][WT] = {};
+    u32x4 av[2][WM];
+    f32x4 scale[SG][WM];
+    Step f;
+    auto operands = [&](int buf) SAMD_INLINE {   // of W, and the scales
 #pragma unroll
         for (int i = 0; i < WM; ++i) {
-            const f32x4 f = *(const f32x4 *)&ss[buf][c * BM + (mw * WM + i) * 16 + quarter * 4];
 #pragma unroll
-            for (int t = 0; t < WT; ++t) {
+            for (int c = 0; c < 2; ++c) av[c][i] = ws[buf][(mw * WM + i) * 128 + at[c]];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[i][t][r] = fmaf(f[r], sum[i][t][r], acc[i][t][r]);
-                sum[i][t] = f32x4{};
-            }
+            for (int c = 0; c < SG; ++c) scale[c][i] = *(const f32x4 *)&ss[buf][c * BM + (mw * WM + i) * 16 + quarter * 4];
         }
     };
-    auto multiply = [&](int buf, bool last_of_group) {
+    // A step's products with token tiles from .. to - 1.  The sums of a step (of each half where groups are 32) are
+    // scaled at once: they live for a few instructions only.
+    auto multiply = [&](auto &&x_of, int from, int to) SAMD_INLINE {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            u32x4 av[WM];
+        for (int t = from; t < to; ++t) {
+            f32x4 sum[SG][WM] = {};
 #pragma unroll
-            for (int i = 0; i < WM; ++i) av[i] = ws[buf][part_at((mw * WM + i) * 16 + low, c * 4 + quarter)];
-#pragma unroll
-            for (int t = 0; t < WT; ++t)
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
-                    const u32x4 bv = xs[buf][j][part_at((tw * WT + t) * 16 + low, c * 4 + quarter)];
+                    const u32x4 bv = x_of(c, j, t);
 #pragma unroll
-                    for (int i = 0; i < WM; ++i) sum[i][t] = mfma<H>(av[i], bv, sum[i][t]);
+                    for (int i = 0; i < WM; ++i) sum[c % SG][i] = mfma<H>(av[c][i], bv, sum[c % SG][i]);
                 }
-            if (PER == 1) {
-                flush(buf, c);
-                __builtin_amdgcn_sched_barrier(0);   // the halves overlapped would need more registers than there are
-            }
+#pragma unroll
+            for (int c = 0; c < SG; ++c)
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][t][r] = fmaf(scale[c][i][r], sum[c][i][r], acc[i][t][r]);
         }
-        if (PER > 1 && last_of_group) flush(buf, 0);
+#pragma unroll
+        for (int t = from; t < to; ++t)   // here, not behind the barrier, where the sums would still need registers
+#pragma unroll
+            for (int i = 0; i < WM; ++i) asm volatile("" : "+v"(acc[i][t]));
     };
 
-    load(0);
-    store(0, 0);
+    // Two steps a turn, so that the buffers are known.  The slices take turns in turn, all as many (steps behind
+    // the last are zeros).
+    const int turns = (steps + 2 * KS - 1) / (2 * KS);
+    constexpr int NEXT = 2 * KS;
+    int step = 2 * slice;
+    load(f, step);
+    store(std::true_type{}, f, step, 0);
+    load(f, step + 1);
     __syncthreads();
-    // two steps a turn: the buffers are known, and a group of 128 ends with the second (steps behind the last are zeros)
-    for (int step = 0; step < steps; step += 2) {
-        load(step + 1);
-        multiply(0, PER == 2);
-        store(step + 1, 1);
+    auto all_turns = [&](auto &&one) SAMD_INLINE {
+        int turn = 0;
+        for (; turn < turns && step + NEXT < p.K / kGemmStep; ++turn, step += NEXT) one(std::false_type{});
+        for (; turn < turns; ++turn, step += NEXT) one(std::true_type{});
+    };
+    if constexpr (KS == 1 && TW * MW == 8) {
+        // Eight waves, two on each SIMD: the second four run one phase behind the first, so that one wave of a
+        // SIMD multiplies while the other fetches its operands and decodes.
+        const bool behind = wave >= 4;
+        u32x4 bv[2][P][WT];
+        auto fetch = [&](auto ragged, int buf, int next) SAMD_INLINE {
+            operands(buf);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < P; ++j)
+#pragma unroll
+                    for (int t = 0; t < WT; ++t) bv[c][j][t] = xs[buf][j][(tw * WT + t) * 128 + at[c]];
+            store(ragged, f, next, buf ^ 1);
+            load(f, next + 1);
+            __syncthreads();
+            __builtin_amdgcn_s_setprio(1);
+            multiply([&](int c, int j, int t) SAMD_INLINE { return bv[c][j][t]; }, 0, WT);
+            __builtin_amdgcn_s_setprio(0);
+            __syncthreads();
+        };
+        if (behind) __syncthreads();
+        all_turns([&](auto ragged) SAMD_INLINE {
+            fetch(ragged, 0, step + 1);
+            fetch(ragged, 1, step + 2);
+        });
+        if (!behind) __syncthreads();
+    } else {
+        // The next step's data goes into the other buffer between the products of the two halves of the tokens.
+        auto both = [&](auto ragged, int buf, int next, int after) SAMD_INLINE {
+            auto x_of = [&](int c, int j, int t) SAMD_INLINE { return xs[buf][j][(tw * WT + t) * 128 + at[c]]; };
+            operands(buf);
+            multiply(x_of, 0, WT / 2);
+            store(ragged, f, next, buf ^ 1);
+            multiply(x_of, WT / 2, WT);
+            load(f, after);
+            __syncthreads();
+        };
+        all_turns([&](auto ragged) SAMD_INLINE {
+            both(ragged, 0, step + 1, step + NEXT);
+            both(ragged, 1, step + NEXT, step + NEXT + 1);
+        });
+    }
+    if constexpr (KS > 1) {   // the first slice's waves add the others' sums, in order
+        f32x4 *meet = (f32x4 *)all;
+        auto at_sum = [&](int from, int i, int t) { return ((((from - 1) * TW * MW + wave) * WM + i) * WT + t) * 64 + lane; };
+        if (slice)
+#pragma unroll
+            for (int i = 0; i < WM; ++i)
+#pragma unroll
+                for (int t = 0; t < WT; ++t) meet[at_sum(slice, i, t)] = acc[i][t];
         __syncthreads();
-        load(step + 2);
-        multiply(1, true);
-        store(step + 2, 0);
-        __syncthreads();
+        if (slice) return;
+        for (int from = 1; from < KS; ++from)
+#pragma unroll
+            for (int i = 0; i < WM; ++i)
+#pragma unroll
+                for (int t = 0; t < WT; ++t) acc[i][t] += meet[at_sum(from, i, t)];
     }
 
 #pragma unroll
@@ -294,7 +372,7 @@ __global__ __launch_bounds__(64 * TW * MW) void group_gemm_kernel(GroupProduct p
     }
 }
 
-template <class X, int NW, int WT, int WM, int TW, int MW>
+template <class X, bool BUF, int NW, int WT, int WM, int TW, int MW, int KS>
 int launch_gemm_tile(const GroupProduct &p, int words, int groups, hipStream_t s) {
     constexpr int BT = 16 * WT * TW, OM = 16 * WM * MW / NW;
     const int64_t tblocks = ((int64_t)p.T + BT - 1) / BT, blocks = tblocks * (((int64_t)p.M + OM - 1) / OM);
@@ -302,11 +380,10 @@ int launch_gemm_tile(const GroupProduct &p, int words, int groups, hipStream_t s
         set_error("group product: T x M needs too many workgroups");
         return SAMD_EUNSUPPORTED;
     }
-    const bool buffered = within_buffer(p.x, sizeof(X), std::min<int64_t>(p.T, BT), p.ldx, p.K);
     const bool vecy = rows4(p.y, p.type, p.ldy);
     auto go = [&](auto per) {
-        hipLaunchKernelGGL((group_gemm_kernel<X, decltype(per)::value, NW, WT, WM, TW, MW>), dim3((uint32_t)blocks),
-                           dim3(64 * TW * MW), 0, s, p, words, groups, (int)tblocks, buffered, vecy);
+        hipLaunchKernelGGL((group_gemm_kernel<X, BUF, decltype(per)::value, NW, WT, WM, TW, MW, KS>), dim3((uint32_t)blocks),
+                           dim3(64 * TW * MW * KS), 0, s, p, words, groups, (int)tblocks, vecy);
     };
     if (p.group == 32) go(std::integral_constant<int, 1>{});
     else if (p.group == 64) go(std::integral_constant<int, 2>{});

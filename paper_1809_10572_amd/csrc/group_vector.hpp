@@ -97,17 +97,16 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
     auto fetch = [&](int step, Step &f) {
         // always requested, so that the wait for a step's weights leaves the next step's in flight; a step
         // behind the last is asked for behind the buffer's end, which reads no memory
-        const uint32_t at = step < steps ? (uint32_t)(step * 1024 + lane * 16) : 0x80000000u;
+        const uint32_t at = step < steps ? (uint32_t)(step * 1024 + lane * 16) : 0xc0000000u;
         const uint32_t g = (uint32_t)min((step * kVecStep + lane * 32) >> gshift, groups - 1);
 #pragma unroll
         for (int a = 0; a < NW; ++a)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                f.w[a][r] = __builtin_amdgcn_raw_buffer_load_b128(rq[a], at, (uint32_t)r * (uint32_t)words * 4u, 0);
-                f.s[a][r] = __uint_as_float(
-                    __builtin_amdgcn_raw_buffer_load_b32(rs[a], g * 4, (uint32_t)r * (uint32_t)groups * 4u, 0));
-                if (!SIGNED)
-                    f.z[a][r] = __builtin_amdgcn_raw_buffer_load_b8(rz[a], g, (uint32_t)r * (uint32_t)groups, 0);
+                f.w[a][r] = __builtin_amdgcn_raw_buffer_load_b128(rq[a], at + (uint32_t)r * (uint32_t)words * 4u, 0, 0);
+                f.s[a][r] =
+                    __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs[a], (g + (uint32_t)r * (uint32_t)groups) * 4, 0, 0));
+                if (!SIGNED) f.z[a][r] = __builtin_amdgcn_raw_buffer_load_b8(rz[a], g + (uint32_t)r * (uint32_t)groups, 0, 0);
             }
     };
     float acc[NW][R][T] = {};
@@ -127,7 +126,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
                 for (int r = 0; r < R; ++r) {
                     if constexpr (kWide) {
                         const uint32_t w = SIGNED ? f.w[a][r][i] ^ 0x88888888u : f.w[a][r][i];
-                        const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
+                        const uint32_t lo = as_is(w & 0x0f0f0f0fu), hi = as_is((w >> 4) & 0x0f0f0f0fu);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float e = (float)((lo >> (8 * j)) & 255u), o = (float)((hi >> (8 * j)) & 255u);

@@ -187,7 +187,7 @@ int launch_relu_requant_nhwc_u8(const int32_t *acc, int N, int C, int H, int W, 
                                 int bits, uint8_t *dst, hipStream_t s);
 
 // Group-scaled rows (arguments checked by the callers in api.cpp).
-constexpr int64_t kMaxGroupCols = (int64_t)1 << 27;   // longest row of weights in a product
+constexpr int64_t kMaxGroupCols = (int64_t)1 << 25;   // longest row of weights in a product: 128 of them are 2 GB
 struct GroupW {              // one group-scaled tensor
     const uint32_t *q;
     const float *scale;

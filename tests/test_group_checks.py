@@ -88,6 +88,8 @@ def test_products_refuse(call):
         assert call(**{size: -1}) == EINVAL and call(**{size: 1 << 31}) == EINVAL
     assert b"2^31 - 1" in samd.lib().samd_last_error()
     assert call(wf=U4) == EINVAL                     # unsigned without zero points
+    wide = (1 << 25) + 1
+    assert call(K=wide, **({"lddx": wide} if call is grad else {"ldx": wide})) == EUNSUP
     assert call(T=0) == OK                           # nothing to do
 
 
