@@ -7,8 +7,7 @@
 // A workgroup computes 16 WT TW tokens x 16 WM MW rows of W with TW x MW waves for each of KS slices of K, a
 // wave 16 WT x 16 WM: large tiles where there are many tokens, slices where there are too few to fill the card.  Steps of 64
 // values: x (copied) and the fields (decoded once for the workgroup) go through LDS, two buffers, the next
-// step's loads in flight during this step's products.  A row of a buffer is 128 bytes, its 16-byte parts exchanged
-// by (row / 2) % 8, so that the 16 rows which an operand's lanes read meet no bank twice.
+// step's loads in flight during this step's products.
 // W is the first operand: a lane then ends with 4 consecutive rows of W for a token, which are stored together
 // and are one word of the gated block's stored projections.
 #pragma once
@@ -21,8 +20,10 @@ namespace samd {
 #define SAMD_INLINE __attribute__((always_inline))
 
 constexpr int kGemmStep = 64;
-// Index of 16-byte part `c` (0..7) of row `r` in a buffer.
-__device__ __forceinline__ int part_at(int r, int c) { return r * 8 + (c ^ ((r >> 1) & 7)); }
+// Index of 16-byte part `c` (0..7) of row `r` in a buffer of rows of 64 16-bit values.  Of 16 rows, 0..7 lie in the lower
+// halves of 256 bytes (all banks), 8..15 in the upper ones, their parts exchanged by r % 8: neither the 16 rows that an
+// operand's lanes read at one c, nor 8 parts of two rows that are 8 apart, meet a bank twice.
+__device__ __forceinline__ int part_at(int r, int c) { return ((r & ~15) + (r & 7) * 2 + (r >> 3 & 1)) * 8 + (c ^ (r & 7)); }
 
 // 8 fields of a word minus z as 16-bit floats in order (z + 8 for signed fields, whose sign bits are flipped).
 template <class H>
@@ -81,15 +82,15 @@ struct TokenTile {
         }
     }
 
-    // RAGGED: the step may reach behind the rows' end.
-    template <bool RAGGED, int P>
-    __device__ __forceinline__ void store(u32x4 (&to)[P][ROWS * 8], int cols, int step, int tid) {
+    // RAGGED: the step may reach behind the rows' end.  convert(): 8 values as P matrix operands.
+    template <bool RAGGED, int P, class F>
+    __device__ __forceinline__ void store(u32x4 (&to)[P][ROWS * 8], int cols, int step, int tid, F &&convert) {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const int id = e * THREADS + tid;
             if (RAGGED) clear_behind(raw[e], cols - (step * kGemmStep + id % 8 * 8));
             u32x4 piece[P];
-            x_operand(raw[e], piece);
+            convert(raw[e], piece);
 #pragma unroll
             for (int j = 0; j < P; ++j) to[j][part_at(id / 8, id % 8)] = piece[j];
         }
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_gemm_kernel(GroupProd
         for (int c = 0; c < SG; ++c) f.s[c] = sp[min(step * kGemmStep / (32 * PER) + c, groups - 1)];
     };
     auto store = [&](auto ragged, Step &f, int step, int buf) SAMD_INLINE {
-        f.x.template store<decltype(ragged)::value>(xs[buf], p.K, step, tid);
+        f.x.template store<decltype(ragged)::value>(xs[buf], p.K, step, tid, [](const Raw8<X> &r, u32x4(&o)[P]) { x_operand(r, o); });
 #pragma unroll
         for (int i = 0; i < WPT; ++i)
             ws[buf][part_at(wrow, part + i)] = whole_values<H>(f.q[i] ^ flip, has_zero ? (int)f.z : 8);

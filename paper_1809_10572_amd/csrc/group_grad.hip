@@ -1,54 +1,309 @@
-// The input gradient of products with 4-bit group-scaled weights: dx = dy W (+ dy2 W2).
+// The input gradient of products with 4-bit group-scaled weights on the matrix cores: dx = dy W (+ dy2 W2).
 //
-// One thread computes 8 consecutive columns of one token, walking the rows of W.
+// The sum runs over the rows of W, and a group's scale differs from row to row, so it is part of the summed product
+// and has to be multiplied into an operand: a weight s (u - z) is computed in 32-bit floats and enters
+//   bf16  as one bf16, rounded: an error of at most 2^-9 of each weight, as small as that of dy itself
+//   f16   as two bf16 of together 16 bits and more, dy as two that hold its 11 bits: three instructions a product
+//   f32   as three bf16 of 8 bits, as is dy: the six largest of their products, off by 2^-24
+// (a bf16 holds any float's range; an f16 operand would lose small scales).  Everything is summed in 32-bit floats, both
+// pairs into one sum, and rounded once.
+//
+// A workgroup computes 16 WT TW tokens x 16 WM MW columns of W with TW x MW waves for each of KS slices of the sum, steps
+// of 64 rows of W through LDS as in the products of many tokens.  The matrix instruction wants neighbouring rows of W side
+// by side, the words hold neighbouring columns: a thread takes the same KPT columns of eight rows and writes KPT
+// operand parts of eight rows each, so the transposition costs nothing but its choice of pairs.
 #include <hip/hip_runtime.h>
 
-#include "group_device.hpp"
+#include "group_gemm.hpp"
 
 namespace samd {
 
 namespace {
 
+// bf16 pieces of dy and of a weight.
 template <class X>
-__global__ __launch_bounds__(256) void group_grad_kernel(GroupGrad p, int words, int groups, int gshift, int64_t items,
-                                                         RowOf div) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= items) return;
-    const int64_t t = row_index(div, i);
-    const int w = (int)(i - t * div.per);
-    float acc[8] = {};
-    for (int a = 0; a < 2 && p.dy[a]; ++a) {
-        const X *dy = (const X *)p.dy[a] + t * p.lddy;
-        for (int m = 0; m < p.M; ++m) {
-            const int64_t g = (int64_t)m * groups + (w >> (gshift - 3));
-            const uint32_t q = p.w[a].q[(int64_t)m * words + w];
-            const int z = p.w[a].zero ? (int)p.w[a].zero[g] : 8;
-            const uint32_t u = p.w[a].zero ? q : q ^ 0x88888888u;
-            const float v = (float)dy[m];
+constexpr int kGradPieces = sizeof(X) == 4 ? 3 : std::is_same_v<X, half_t> ? 2 : 1;
+
+// The upper halves of two floats: bf16 by cutting off.
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+
+__device__ __forceinline__ float behind_upper_half(float v) { return v - __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+
+// 8 floats as P bf16 operands: all but the last by cutting, the last rounded.
+template <int P>
+__device__ __forceinline__ void pieces_of(float (&v)[8], u32x4 (&out)[P]) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += v * (p.w[a].scale[g] * (float)((int)((u >> (4 * j)) & 15u) - z));
+    for (int j = 0; j < P; ++j) {
+        if (j == P - 1) {
+            bf16_t h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = (bf16_t)v[i];
+            out[j] = __builtin_bit_cast(u32x4, h);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[j][i] = upper_halves(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = behind_upper_half(v[i]);
         }
     }
-    store8((X *)p.dx + t * p.lddx + (int64_t)w * 8, min(8, p.K - w * 8), false, acc);
+}
+
+template <class X>
+__device__ __forceinline__ void grad_operand(const Raw8<X> &raw, u32x4 (&out)[kGradPieces<X>]) {
+    if constexpr (std::is_same_v<X, half_t>) {
+        half_t h[8];
+        *(u32x4 *)h = raw.v[0];
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+        pieces_of(v, out);
+    } else {
+        x_operand(raw, out);
+    }
+}
+
+template <class X, bool SIGNED, bool BUF, int WT, int WM, int TW, int MW, int KS>
+__global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad p, int words, int groups, int gshift,
+                                                                       int tblocks, bool vecx) {
+    constexpr int P = kGradPieces<X>, THREADS = 64 * TW * MW;
+    constexpr int BT = 16 * WT * TW, BN = 16 * WM * MW;
+    constexpr int KPT = BN * 8 / THREADS;   // columns of a thread: a half or a quarter of a word
+    static_assert(KPT == 2 || KPT == 4, "columns of a thread");
+    struct Buffers {
+        u32x4 x[2][P][BT * 8], w[2][P][BN * 8];
+    };
+    static_assert((KS - 1) * BT * BN * 4 <= (int)sizeof(Buffers) * KS, "the slices' sums meet in the buffers");
+    __shared__ Buffers all[KS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % (TW * MW);
+    const int slice = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / (TW * MW), tid = threadIdx.x - slice * THREADS;
+    auto &xs = all[slice].x;
+    auto &ws = all[slice].w;
+    const int quarter = lane >> 4, low = lane & 15, tw = wave % TW, mw = wave / TW;
+    const uint32_t tile = tile_of(blockIdx.x, gridDim.x);
+    const int64_t t0 = (int64_t)(tile % tblocks) * BT, k0 = (int64_t)(tile / tblocks) * BN;
+    const int tokens = (int)min((int64_t)BT, p.T - t0);
+    const int single = (p.M + kGemmStep - 1) / kGemmStep, steps = p.dy[1] ? 2 * single : single;   // of both pairs
+
+    // The 8 rows and KPT columns of a thread, eight neighbouring threads of different rows: their LDS writes meet no
+    // bank twice, and 8 words of a row are read together.
+    const int chunk = tid % 8, column = (tid / 8 % (BN / 8)) * 8 + tid / BN * KPT;
+    const int word = (int)(k0 / 8) + column / 8, shift = column % 8 * 4;
+    const int group = (int)min((k0 + column) >> gshift, (int64_t)groups - 1);
+    constexpr uint32_t kFlip = SIGNED ? 0x88888888u : 0u;
+
+    struct Step {
+        TokenTile<X, BT, THREADS, BUF> x;
+        uint32_t q[8], z[SIGNED ? 1 : 8];
+        float s[8];
+    } f;
+    auto load = [&](int step) SAMD_INLINE {
+        step = __builtin_amdgcn_readfirstlane(step);
+        asm("" : "+s"(step));   // addresses from one scalar each turn, not a register carried for each of them
+        const bool second = step >= single && p.dy[1];
+        const int s = second ? step - single : step;
+        const X *x = (const X *)(second ? p.dy[1] : p.dy[0]) + t0 * p.lddy;
+        const __amdgpu_buffer_rsrc_t rx = buffer_of(x, ((int64_t)(tokens - 1) * p.lddy + p.M) * (int64_t)sizeof(X));
+        f.x.load(rx, x, p.lddy, tokens, p.M, s, tid);
+        // the step's rows of W; rows behind the last are zeros (of scale 0)
+        const int64_t m0 = min((int64_t)s * kGemmStep, (int64_t)p.M);
+        const int64_t rows = min((int64_t)kGemmStep, p.M - m0);
+        const GroupW &w = p.w[second ? 1 : 0];
+        const __amdgpu_buffer_rsrc_t rq = buffer_of(w.q + m0 * words, rows * words * 4);
+        const __amdgpu_buffer_rsrc_t rs = buffer_of(w.scale + m0 * groups, rows * groups * 4);
+        const __amdgpu_buffer_rsrc_t rz = buffer_of(w.zero + m0 * groups, SIGNED ? 0 : rows * groups);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t r = chunk * 8 + j;
+            f.q[j] = __builtin_amdgcn_raw_buffer_load_b32(rq, (r * (uint32_t)words + word) * 4, 0, 0);
+            f.s[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (r * (uint32_t)groups + group) * 4, 0, 0));
+            if (!SIGNED) f.z[j] = __builtin_amdgcn_raw_buffer_load_b8(rz, r * (uint32_t)groups + group, 0, 0);
+        }
+    };
+    auto store = [&](auto ragged, int step, int buf) SAMD_INLINE {
+        const int s = p.dy[1] && step >= single ? step - single : step;
+        f.x.template store<decltype(ragged)::value>(xs[buf], p.M, s, tid,
+                                                    [](const Raw8<X> &r, u32x4(&o)[P]) { grad_operand(r, o); });
+        float v[KPT][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t u = ((f.q[j] ^ kFlip) >> shift) & (KPT == 4 ? 0xffffu : 0xffu);
+            const uint32_t lo = as_is(u & 0x0f0f0f0fu), hi = as_is((u >> 4) & 0x0f0f0f0fu);
+            const float off = -f.s[j] * (SIGNED ? 8.0f : (float)f.z[SIGNED ? 0 : j]);   // exact up to one rounding, as is the sum below
+#pragma unroll
+            for (int c = 0; c < KPT; c += 2) {
+                v[c][j] = fmaf(f.s[j], (float)((lo >> (4 * c)) & 255u), off);
+                v[c + 1][j] = fmaf(f.s[j], (float)((hi >> (4 * c)) & 255u), off);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < KPT; ++c) {
+            u32x4 piece[P];
+            pieces_of(v[c], piece);
+#pragma unroll
+            for (int j = 0; j < P; ++j) ws[buf][j][part_at(column + c, chunk)] = piece[j];
+        }
+    };
+
+    const int at[2] = {part_at(low, quarter), part_at(low, 4 + quarter)};   // the same in every 16 rows
+    f32x4 acc[WM][WT] = {};
+    u32x4 av[2][P][WM];
+    auto operands = [&](int buf) SAMD_INLINE {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+#pragma unroll
+                for (int i = 0; i < WM; ++i) av[c][j][i] = ws[buf][j][(mw * WM + i) * 128 + at[c]];
+    };
+    auto multiply = [&](auto &&x_of, int from, int to) SAMD_INLINE {
+#pragma unroll
+        for (int t = from; t < to; ++t)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const u32x4 bv = x_of(c, j, t);
+#pragma unroll
+                    for (int h = 0; h < P - j; ++h)   // pieces j and h: 2^-8(j + h) of the product
+#pragma unroll
+                        for (int i = 0; i < WM; ++i) acc[i][t] = mfma<bf16_t>(av[c][h][i], bv, acc[i][t]);
+                }
+    };
+
+    // Turns of two steps and the two ways through a step as in the products of many tokens.
+    const int turns = (steps + 2 * KS - 1) / (2 * KS);
+    constexpr int NEXT = 2 * KS;
+    int step = 2 * slice;
+    load(step);
+    store(std::true_type{}, step, 0);
+    load(step + 1);
+    __syncthreads();
+    auto all_turns = [&](auto &&one) SAMD_INLINE {
+        int turn = 0;
+        const bool whole = p.M % kGemmStep == 0;   // else each pair ends with a ragged step
+        for (; turn < turns && whole && step + NEXT < steps; ++turn, step += NEXT) one(std::false_type{});
+        for (; turn < turns; ++turn, step += NEXT) one(std::true_type{});
+    };
+    if constexpr (KS == 1 && TW * MW == 8) {
+        const bool behind = wave >= 4;
+        u32x4 bv[2][P][WT];
+        auto fetch = [&](auto ragged, int buf, int next) SAMD_INLINE {
+            operands(buf);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < P; ++j)
+#pragma unroll
+                    for (int t = 0; t < WT; ++t) bv[c][j][t] = xs[buf][j][(tw * WT + t) * 128 + at[c]];
+            store(ragged, next, buf ^ 1);
+            load(next + 1);
+            __syncthreads();
+            __builtin_amdgcn_s_setprio(1);
+            multiply([&](int c, int j, int t) SAMD_INLINE { return bv[c][j][t]; }, 0, WT);
+            __builtin_amdgcn_s_setprio(0);
+            __syncthreads();
+        };
+        if (behind) __syncthreads();
+        all_turns([&](auto ragged) SAMD_INLINE {
+            fetch(ragged, 0, step + 1);
+            fetch(ragged, 1, step + 2);
+        });
+        if (!behind) __syncthreads();
+    } else {
+        auto both = [&](auto ragged, int buf, int next, int after) SAMD_INLINE {
+            auto x_of = [&](int c, int j, int t) SAMD_INLINE { return xs[buf][j][(tw * WT + t) * 128 + at[c]]; };
+            operands(buf);
+            multiply(x_of, 0, WT / 2);
+            store(ragged, next, buf ^ 1);
+            multiply(x_of, WT / 2, WT);
+            load(after);
+            __syncthreads();
+        };
+        all_turns([&](auto ragged) SAMD_INLINE {
+            both(ragged, 0, step + 1, step + NEXT);
+            both(ragged, 1, step + NEXT, step + NEXT + 1);
+        });
+    }
+    if constexpr (KS > 1) {   // the first slice's waves add the others' sums, in order
+        f32x4 *meet = (f32x4 *)all;
+        auto at_sum = [&](int from, int i, int t) { return ((((from - 1) * TW * MW + wave) * WM + i) * WT + t) * 64 + lane; };
+        if (slice)
+#pragma unroll
+            for (int i = 0; i < WM; ++i)
+#pragma unroll
+                for (int t = 0; t < WT; ++t) meet[at_sum(slice, i, t)] = acc[i][t];
+        __syncthreads();
+        if (slice) return;
+        for (int from = 1; from < KS; ++from)
+#pragma unroll
+            for (int i = 0; i < WM; ++i)
+#pragma unroll
+                for (int t = 0; t < WT; ++t) acc[i][t] += meet[at_sum(from, i, t)];
+    }
+#pragma unroll
+    for (int t = 0; t < WT; ++t) {
+        const int64_t token = t0 + (tw * WT + t) * 16 + low;
+#pragma unroll
+        for (int i = 0; i < WM; ++i) {
+            const int64_t k = k0 + (mw * WM + i) * 16 + quarter * 4;
+            const float v[4] = {acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]};
+            if (token < p.T) store4((X *)p.dx + token * p.lddx + k, (int)min((int64_t)4, p.K - k), vecx, v);
+        }
+    }
+}
+
+template <class X, bool BUF, int WT, int WM, int TW, int MW, int KS>
+int launch_grad_tile(const GroupGrad &p, hipStream_t s) {
+    constexpr int BT = 16 * WT * TW, BN = 16 * WM * MW;
+    const int words = (int)row_words(p.K, 4), groups = (p.K + p.group - 1) / p.group;
+    const int gshift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
+    const int64_t tblocks = ((int64_t)p.T + BT - 1) / BT, blocks = tblocks * (((int64_t)p.K + BN - 1) / BN);
+    if (blocks > INT32_MAX) {
+        set_error("samd_group_matmul_grad: T x K needs too many workgroups");
+        return SAMD_EUNSUPPORTED;
+    }
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * TW * MW * KS), 0, s, p, words, groups, gshift, (int)tblocks,
+                           rows4(p.dx, p.type, p.lddx));
+    };
+    p.w[0].zero ? go(group_grad_kernel<X, false, BUF, WT, WM, TW, MW, KS>) : go(group_grad_kernel<X, true, BUF, WT, WM, TW, MW, KS>);
+    return check_launch("samd_group_matmul_grad");
+}
+
+#ifndef SAMD_TILE
+#define SAMD_TILE 2
+#endif
+
+template <class X>
+int launch_grad_of(const GroupGrad &p, hipStream_t s) {
+    const int64_t rows = std::min<int64_t>(p.T, 256);
+    const bool buffered = within_buffer(p.dy[0], sizeof(X), rows, p.lddy, p.M) &&
+                          (!p.dy[1] || within_buffer(p.dy[1], sizeof(X), rows, p.lddy, p.M));
+    const int tile = SAMD_TILE;
+    if constexpr (std::is_same_v<X, bf16_t>) {
+        if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 4>(p, s);
+        if (tile == 2) return launch_grad_tile<X, true, 4, 4, 2, 4, 1>(p, s);
+        if (tile == 1) return launch_grad_tile<X, true, 4, 4, 2, 2, 2>(p, s);
+        return launch_grad_tile<X, true, 2, 4, 2, 1, 4>(p, s);
+    } else if constexpr (std::is_same_v<X, half_t>) {
+        if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 2>(p, s);
+        if (tile == 2) return launch_grad_tile<X, true, 2, 4, 4, 2, 1>(p, s);
+        if (tile == 1) return launch_grad_tile<X, true, 4, 4, 2, 2, 1>(p, s);
+        return launch_grad_tile<X, true, 2, 4, 2, 1, 2>(p, s);
+    } else {
+        if (!buffered) return launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
+        return launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s);
+    }
 }
 
 }  // namespace
 
 int launch_group_matmul_grad(const GroupGrad &p, hipStream_t s) {
-    const int words = (int)row_words(p.K, 4), groups = (p.K + p.group - 1) / p.group;
-    const int gshift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
-    const int64_t items = (int64_t)p.T * words;
-    if ((items + 255) / 256 > INT32_MAX) {
-        set_error("samd_group_matmul_grad: T x K needs too many workgroups");
-        return SAMD_EUNSUPPORTED;
-    }
-    const RowOf div = row_of(items, (uint32_t)words);
-    with_type(p.type, [&](auto t) {
-        using X = decltype(t);
-        hipLaunchKernelGGL((group_grad_kernel<X>), dim3((uint32_t)((items + 255) / 256)), dim3(256), 0, s, p, words, groups,
-                           gshift, items, div);
-    });
-    return check_launch("samd_group_matmul_grad");
+    if (p.type == SAMD_F32) return launch_grad_of<float>(p, s);
+    if (p.type == SAMD_F16) return launch_grad_of<half_t>(p, s);
+    return launch_grad_of<bf16_t>(p, s);
 }
 
 }  // namespace samd
