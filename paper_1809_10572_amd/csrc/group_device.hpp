@@ -9,6 +9,7 @@ typedef _Float16 half_t;
 typedef __bf16 bf16_t;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef half_t half2_t __attribute__((ext_vector_type(2)));
 typedef bf16_t bf162_t __attribute__((ext_vector_type(2)));

@@ -10,8 +10,10 @@
 //
 // A workgroup computes 16 WT TW tokens x 16 WM MW columns of W with TW x MW waves for each of KS slices of the sum, steps
 // of 64 rows of W through LDS as in the products of many tokens.  The matrix instruction wants neighbouring rows of W side
-// by side, the words hold neighbouring columns: a thread takes the same KPT columns of eight rows and writes KPT
-// operand parts of eight rows each, so the transposition costs nothing but its choice of pairs.
+// by side, the words hold neighbouring columns: the words go into LDS as they are (read straight into the threads that
+// decode them, each row of each word and its scale was a load: 168 us instead of XX for 2048 x 4096 x 4096), and a
+// thread then takes the same KPT columns of eight rows and writes KPT operand parts of eight rows each, so that
+// the transposition costs nothing but its choice of pairs.
 #include <hip/hip_runtime.h>
 
 #include "group_gemm.hpp"
@@ -71,8 +73,11 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     constexpr int BT = 16 * WT * TW, BN = 16 * WM * MW;
     constexpr int KPT = BN * 8 / THREADS;   // columns of a thread: a half or a quarter of a word
     static_assert(KPT == 2 || KPT == 4, "columns of a thread");
+    constexpr int WORDS = BN / 8, GROUPS = BN / 32;   // of a row of the tile; the most groups
     struct Buffers {
         u32x4 x[2][P][BT * 8], w[2][P][BN * 8];
+        u32x4 q[2][kGemmStep * WORDS / 4];        // words as they are stored, 64 rows
+        f32x2 s[2][kGemmStep * GROUPS];           // scales, and scales times zero points
     };
     static_assert((KS - 1) * BT * BN * 4 <= (int)sizeof(Buffers) * KS, "the slices' sums meet in the buffers");
     __shared__ Buffers all[KS];
@@ -86,55 +91,57 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     const int tokens = (int)min((int64_t)BT, p.T - t0);
     const int single = (p.M + kGemmStep - 1) / kGemmStep, steps = p.dy[1] ? 2 * single : single;   // of both pairs
 
-    // The 8 rows and KPT columns of a thread, eight neighbouring threads of different rows: their LDS writes meet no
-    // bank twice, and 8 words of a row are read together.
-    const int chunk = tid % 8, column = (tid / 8 % (BN / 8)) * 8 + tid / BN * KPT;
-    const int word = (int)(k0 / 8) + column / 8, shift = column % 8 * 4;
-    const int group = (int)min((k0 + column) >> gshift, (int64_t)groups - 1);
+    // Position n of a slice is a step of both pairs' rows; those behind the last are zeros.
+    auto step_of = [&](int n) { return __builtin_amdgcn_readfirstlane(2 * slice + n / 2 * 2 * KS + n % 2); };
     constexpr uint32_t kFlip = SIGNED ? 0x88888888u : 0u;
 
-    struct Step {
-        TokenTile<X, BT, THREADS, BUF> x;
-        uint32_t q[8], z[SIGNED ? 1 : 8];
-        float s[8];
-    } f;
-    auto load = [&](int step) SAMD_INLINE {
-        step = __builtin_amdgcn_readfirstlane(step);
+    // On the way in, a thread takes four neighbouring words of a row and the scale of a row and group.
+    constexpr int UNITS = kGemmStep * WORDS / 4;
+    const int urow = tid % UNITS / (WORDS / 4), ucol = tid % (WORDS / 4);
+    const int tile_groups = max(1, BN >> gshift), g0 = (int)(k0 >> gshift);
+    const int srow = tid % kGemmStep, sgroup = min(tid / kGemmStep, tile_groups - 1);
+    struct Words {
+        u32x4 q;
+        float s;
+        uint32_t z;
+    } fw;
+    auto load_words = [&](int n) SAMD_INLINE {
+        int step = step_of(n);
         asm("" : "+s"(step));   // addresses from one scalar each turn, not a register carried for each of them
         const bool second = step >= single && p.dy[1];
-        const int s = second ? step - single : step;
-        const X *x = (const X *)(second ? p.dy[1] : p.dy[0]) + t0 * p.lddy;
-        const __amdgpu_buffer_rsrc_t rx = buffer_of(x, ((int64_t)(tokens - 1) * p.lddy + p.M) * (int64_t)sizeof(X));
-        f.x.load(rx, x, p.lddy, tokens, p.M, s, tid);
-        // the step's rows of W; rows behind the last are zeros (of scale 0)
-        const int64_t m0 = min((int64_t)s * kGemmStep, (int64_t)p.M);
+        // the step's rows of W; rows behind the last read as zeros (of scale 0)
+        const int64_t m0 = min((int64_t)(second ? step - single : step) * kGemmStep, (int64_t)p.M);
         const int64_t rows = min((int64_t)kGemmStep, p.M - m0);
         const GroupW &w = p.w[second ? 1 : 0];
         const __amdgpu_buffer_rsrc_t rq = buffer_of(w.q + m0 * words, rows * words * 4);
         const __amdgpu_buffer_rsrc_t rs = buffer_of(w.scale + m0 * groups, rows * groups * 4);
         const __amdgpu_buffer_rsrc_t rz = buffer_of(w.zero + m0 * groups, SIGNED ? 0 : rows * groups);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t r = chunk * 8 + j;
-            f.q[j] = __builtin_amdgcn_raw_buffer_load_b32(rq, (r * (uint32_t)words + word) * 4, 0, 0);
-            f.s[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (r * (uint32_t)groups + group) * 4, 0, 0));
-            if (!SIGNED) f.z[j] = __builtin_amdgcn_raw_buffer_load_b8(rz, r * (uint32_t)groups + group, 0, 0);
-        }
+        fw.q = __builtin_amdgcn_raw_buffer_load_b128(rq, ((uint32_t)urow * (uint32_t)words + (uint32_t)(k0 / 8) + ucol * 4) * 4, 0, 0);
+        const uint32_t g = (uint32_t)srow * (uint32_t)groups + (uint32_t)min(g0 + sgroup, groups - 1);
+        fw.s = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, g * 4, 0, 0));
+        if (!SIGNED) fw.z = __builtin_amdgcn_raw_buffer_load_b8(rz, g, 0, 0);
     };
-    auto store = [&](auto ragged, int step, int buf) SAMD_INLINE {
-        const int s = p.dy[1] && step >= single ? step - single : step;
-        f.x.template store<decltype(ragged)::value>(xs[buf], p.M, s, tid,
-                                                    [](const Raw8<X> &r, u32x4(&o)[P]) { grad_operand(r, o); });
+    // The words' 16-byte parts exchanged by row / 8, the scales by row % 8 and row / 8: the reads below meet few banks twice.
+    auto store_words = [&](int buf) SAMD_INLINE {
+        all[slice].q[buf][urow * (WORDS / 4) + (ucol ^ (urow / 8 % (WORDS / 4)))] = fw.q;
+        all[slice].s[buf][(srow % 8 * 8 + srow / 8) * GROUPS + sgroup] = f32x2{fw.s, fw.s * (SIGNED ? 8.0f : (float)fw.z)};
+    };
+    // On to the operands, a thread takes KPT columns of 8 rows; eight neighbouring threads different rows.
+    const int chunk = tid % 8, column = (tid / 8 % WORDS) * 8 + tid / BN * KPT;
+    const int word = column / 8, shift = column % 8 * 4, sgroup_of = column >> gshift;
+    auto decode = [&](int buf) SAMD_INLINE {
         float v[KPT][8];
+        const uint32_t *q = (const uint32_t *)all[slice].q[buf];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t u = ((f.q[j] ^ kFlip) >> shift) & (KPT == 4 ? 0xffffu : 0xffu);
+            const uint32_t w = q[(chunk * 8 + j) * WORDS + (word / 4 ^ chunk % (WORDS / 4)) * 4 + word % 4];
+            const f32x2 s = all[slice].s[buf][(j * 8 + chunk) * GROUPS + sgroup_of];
+            const uint32_t u = ((w ^ kFlip) >> shift) & (KPT == 4 ? 0xffffu : 0xffu);
             const uint32_t lo = as_is(u & 0x0f0f0f0fu), hi = as_is((u >> 4) & 0x0f0f0f0fu);
-            const float off = -f.s[j] * (SIGNED ? 8.0f : (float)f.z[SIGNED ? 0 : j]);   // exact up to one rounding, as is the sum below
 #pragma unroll
             for (int c = 0; c < KPT; c += 2) {
-                v[c][j] = fmaf(f.s[j], (float)((lo >> (4 * c)) & 255u), off);
-                v[c + 1][j] = fmaf(f.s[j], (float)((hi >> (4 * c)) & 255u), off);
+                v[c][j] = fmaf(s[0], (float)((lo >> (4 * c)) & 255u), -s[1]);
+                v[c + 1][j] = fmaf(s[0], (float)((hi >> (4 * c)) & 255u), -s[1]);
             }
         }
 #pragma unroll
@@ -144,6 +151,20 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
 #pragma unroll
             for (int j = 0; j < P; ++j) ws[buf][j][part_at(column + c, chunk)] = piece[j];
         }
+    };
+    TokenTile<X, BT, THREADS, BUF> fx;
+    auto load_x = [&](int n) SAMD_INLINE {
+        int step = step_of(n);
+        asm("" : "+s"(step));
+        const bool second = step >= single && p.dy[1];
+        const X *x = (const X *)(second ? p.dy[1] : p.dy[0]) + t0 * p.lddy;
+        const __amdgpu_buffer_rsrc_t rx = buffer_of(x, ((int64_t)(tokens - 1) * p.lddy + p.M) * (int64_t)sizeof(X));
+        fx.load(rx, x, p.lddy, tokens, p.M, second ? step - single : step, tid);
+    };
+    auto store_x = [&](auto ragged, int n, int buf) SAMD_INLINE {
+        const int step = step_of(n);
+        fx.template store<decltype(ragged)::value>(xs[buf], p.M, p.dy[1] && step >= single ? step - single : step, tid,
+                                                   [](const Raw8<X> &r, u32x4(&o)[P]) { grad_operand(r, o); });
     };
 
     const int at[2] = {part_at(low, quarter), part_at(low, 4 + quarter)};   // the same in every 16 rows
@@ -172,24 +193,38 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
                 }
     };
 
-    // Turns of two steps and the two ways through a step as in the products of many tokens.
+    // Position n's operands are made while those of n - 1 are multiplied, its words come into LDS one position
+    // earlier.  Turns of two positions, so that the buffers are known; all slices take as many.
     const int turns = (steps + 2 * KS - 1) / (2 * KS);
-    constexpr int NEXT = 2 * KS;
-    int step = 2 * slice;
-    load(step);
-    store(std::true_type{}, step, 0);
-    load(step + 1);
+    load_words(0);
+    load_x(0);
+    store_words(0);
+    load_words(1);
+    store_x(std::true_type{}, 0, 0);
+    load_x(1);
+    store_words(1);
+    load_words(2);
     __syncthreads();
+    decode(0);
+    __syncthreads();
+    auto ahead = [&](auto ragged, int n, int buf) SAMD_INLINE {   // while position n, in buffer buf, is multiplied
+        store_x(ragged, n + 1, buf ^ 1);
+        decode(buf ^ 1);
+        store_words(buf);
+        load_x(n + 2);
+        load_words(n + 3);
+    };
     auto all_turns = [&](auto &&one) SAMD_INLINE {
         int turn = 0;
         const bool whole = p.M % kGemmStep == 0;   // else each pair ends with a ragged step
-        for (; turn < turns && whole && step + NEXT < steps; ++turn, step += NEXT) one(std::false_type{});
-        for (; turn < turns; ++turn, step += NEXT) one(std::true_type{});
+        for (; turn < turns && whole && step_of(2 * turn + 2) < steps; ++turn) one(std::false_type{}, 2 * turn);
+        for (; turn < turns; ++turn) one(std::true_type{}, 2 * turn);
     };
     if constexpr (KS == 1 && TW * MW == 8) {
+        // two groups of four waves a phase apart, as in the products of many tokens
         const bool behind = wave >= 4;
         u32x4 bv[2][P][WT];
-        auto fetch = [&](auto ragged, int buf, int next) SAMD_INLINE {
+        auto both = [&](auto ragged, int n, int buf) SAMD_INLINE {
             operands(buf);
 #pragma unroll
             for (int c = 0; c < 2; ++c)
@@ -197,8 +232,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
                 for (int j = 0; j < P; ++j)
 #pragma unroll
                     for (int t = 0; t < WT; ++t) bv[c][j][t] = xs[buf][j][(tw * WT + t) * 128 + at[c]];
-            store(ragged, next, buf ^ 1);
-            load(next + 1);
+            ahead(ragged, n, buf);
             __syncthreads();
             __builtin_amdgcn_s_setprio(1);
             multiply([&](int c, int j, int t) SAMD_INLINE { return bv[c][j][t]; }, 0, WT);
@@ -206,24 +240,23 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
             __syncthreads();
         };
         if (behind) __syncthreads();
-        all_turns([&](auto ragged) SAMD_INLINE {
-            fetch(ragged, 0, step + 1);
-            fetch(ragged, 1, step + 2);
+        all_turns([&](auto ragged, int n) SAMD_INLINE {
+            both(ragged, n, 0);
+            both(ragged, n + 1, 1);
         });
         if (!behind) __syncthreads();
     } else {
-        auto both = [&](auto ragged, int buf, int next, int after) SAMD_INLINE {
+        auto both = [&](auto ragged, int n, int buf) SAMD_INLINE {
             auto x_of = [&](int c, int j, int t) SAMD_INLINE { return xs[buf][j][(tw * WT + t) * 128 + at[c]]; };
             operands(buf);
             multiply(x_of, 0, WT / 2);
-            store(ragged, next, buf ^ 1);
+            ahead(ragged, n, buf);
             multiply(x_of, WT / 2, WT);
-            load(after);
             __syncthreads();
         };
-        all_turns([&](auto ragged) SAMD_INLINE {
-            both(ragged, 0, step + 1, step + NEXT);
-            both(ragged, 1, step + NEXT, step + NEXT + 1);
+        all_turns([&](auto ragged, int n) SAMD_INLINE {
+            both(ragged, n, 0);
+            both(ragged, n + 1, 1);
         });
     }
     if constexpr (KS > 1) {   // the first slice's waves add the others' sums, in order
