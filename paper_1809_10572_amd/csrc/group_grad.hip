@@ -11,7 +11,7 @@
 // A workgroup computes 16 WT TW tokens x 16 WM MW columns of W with TW x MW waves for each of KS slices of the sum, steps
 // of 64 rows of W through LDS as in the products of many tokens.  The matrix instruction wants neighbouring rows of W side
 // by side, the words hold neighbouring columns: the words go into LDS as they are (read straight into the threads that
-// decode them, each row of each word and its scale was a load: 168 us instead of XX for 2048 x 4096 x 4096), and a
+// decode them, each row of each word and its scale was a load: 168 us against 110 for 2048 x 4096 x 4096 bf16, one tile), and a
 // thread then takes the same KPT columns of eight rows and writes KPT operand parts of eight rows each, so that
 // the transposition costs nothing but its choice of pairs.
 #include <hip/hip_runtime.h>
@@ -214,51 +214,22 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
         load_x(n + 2);
         load_words(n + 3);
     };
-    auto all_turns = [&](auto &&one) SAMD_INLINE {
-        int turn = 0;
-        const bool whole = p.M % kGemmStep == 0;   // else each pair ends with a ragged step
-        for (; turn < turns && whole && step_of(2 * turn + 2) < steps; ++turn) one(std::false_type{}, 2 * turn);
-        for (; turn < turns; ++turn) one(std::true_type{}, 2 * turn);
+    auto both = [&](auto ragged, int n, int buf) SAMD_INLINE {
+        auto x_of = [&](int c, int j, int t) SAMD_INLINE { return xs[buf][j][(tw * WT + t) * 128 + at[c]]; };
+        operands(buf);
+        multiply(x_of, 0, WT / 2);
+        ahead(ragged, n, buf);
+        multiply(x_of, WT / 2, WT);
+        __syncthreads();
     };
-    if constexpr (KS == 1 && TW * MW == 8) {
-        // two groups of four waves a phase apart, as in the products of many tokens
-        const bool behind = wave >= 4;
-        u32x4 bv[2][P][WT];
-        auto both = [&](auto ragged, int n, int buf) SAMD_INLINE {
-            operands(buf);
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int j = 0; j < P; ++j)
-#pragma unroll
-                    for (int t = 0; t < WT; ++t) bv[c][j][t] = xs[buf][j][(tw * WT + t) * 128 + at[c]];
-            ahead(ragged, n, buf);
-            __syncthreads();
-            __builtin_amdgcn_s_setprio(1);
-            multiply([&](int c, int j, int t) SAMD_INLINE { return bv[c][j][t]; }, 0, WT);
-            __builtin_amdgcn_s_setprio(0);
-            __syncthreads();
-        };
-        if (behind) __syncthreads();
-        all_turns([&](auto ragged, int n) SAMD_INLINE {
-            both(ragged, n, 0);
-            both(ragged, n + 1, 1);
-        });
-        if (!behind) __syncthreads();
-    } else {
-        auto both = [&](auto ragged, int n, int buf) SAMD_INLINE {
-            auto x_of = [&](int c, int j, int t) SAMD_INLINE { return xs[buf][j][(tw * WT + t) * 128 + at[c]]; };
-            operands(buf);
-            multiply(x_of, 0, WT / 2);
-            ahead(ragged, n, buf);
-            multiply(x_of, WT / 2, WT);
-            __syncthreads();
-        };
-        all_turns([&](auto ragged, int n) SAMD_INLINE {
-            both(ragged, n, 0);
-            both(ragged, n + 1, 1);
-        });
-    }
+    auto turn_of = [&](auto ragged, int n) SAMD_INLINE {
+        both(ragged, n, 0);
+        both(ragged, n + 1, 1);
+    };
+    int turn = 0;
+    const bool whole = p.M % kGemmStep == 0;   // else each pair ends with a ragged step
+    for (; turn < turns && whole && step_of(2 * turn + 2) < steps; ++turn) turn_of(std::false_type{}, 2 * turn);
+    for (; turn < turns; ++turn) turn_of(std::true_type{}, 2 * turn);
     if constexpr (KS > 1) {   // the first slice's waves add the others' sums, in order
         f32x4 *meet = (f32x4 *)all;
         auto at_sum = [&](int from, int i, int t) { return ((((from - 1) * TW * MW + wave) * WM + i) * WT + t) * 64 + lane; };
@@ -305,29 +276,29 @@ int launch_grad_tile(const GroupGrad &p, hipStream_t s) {
     return check_launch("samd_group_matmul_grad");
 }
 
-#ifndef SAMD_TILE
-#define SAMD_TILE 2
-#endif
-
+// A workgroup fills a CU, so a tile costs its time for each round of 256 workgroups; the units are microseconds measured
+// for M = 4096 (they grow with M alike).
 template <class X>
 int launch_grad_of(const GroupGrad &p, hipStream_t s) {
     const int64_t rows = std::min<int64_t>(p.T, 256);
     const bool buffered = within_buffer(p.dy[0], sizeof(X), rows, p.lddy, p.M) &&
                           (!p.dy[1] || within_buffer(p.dy[1], sizeof(X), rows, p.lddy, p.M));
-    const int tile = SAMD_TILE;
+    auto cost = [&](int64_t tokens, int64_t columns, int64_t unit) {
+        const int64_t blocks = ((p.T + tokens - 1) / tokens) * ((p.K + columns - 1) / columns);
+        return (blocks + 255) / 256 * unit;
+    };
     if constexpr (std::is_same_v<X, bf16_t>) {
         if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 4>(p, s);
-        if (tile == 2) return launch_grad_tile<X, true, 4, 4, 2, 4, 1>(p, s);
-        if (tile == 1) return launch_grad_tile<X, true, 4, 4, 2, 2, 2>(p, s);
+        const int64_t small = cost(64, 64, 29), middle = cost(128, 128, 55), large = cost(256, 128, 98);
+        if (large < middle && large < small) return launch_grad_tile<X, true, 4, 4, 4, 2, 1>(p, s);
+        if (middle < small) return launch_grad_tile<X, true, 4, 4, 2, 2, 2>(p, s);
         return launch_grad_tile<X, true, 2, 4, 2, 1, 4>(p, s);
     } else if constexpr (std::is_same_v<X, half_t>) {
         if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 2>(p, s);
-        if (tile == 2) return launch_grad_tile<X, true, 2, 4, 4, 2, 1>(p, s);
-        if (tile == 1) return launch_grad_tile<X, true, 4, 4, 2, 2, 1>(p, s);
+        if (cost(128, 128, 117) < cost(64, 64, 54)) return launch_grad_tile<X, true, 2, 4, 4, 2, 1>(p, s);
         return launch_grad_tile<X, true, 2, 4, 2, 1, 2>(p, s);
     } else {
-        if (!buffered) return launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
-        return launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s);
+        return buffered ? launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s) : launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
     }
 }
 
