@@ -797,10 +797,13 @@ class GroupRows(NamedTuple):
     group: int
 
 
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _launch(fn, t: torch.Tensor, *args) -> None:
     """Call an entry point on t's device and that device's current stream."""
     at = t.get_device()
-    if at < 0 or at == torch.cuda.current_device():
+    if at < 0 or at == _get_device():
         status = fn(*args, _stream(t))
     else:
         with torch.cuda.device(at):
@@ -818,13 +821,14 @@ def _matrix(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> 
         raise ValueError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
     if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} must have the type and device of the other operands")
-    if t.dim() == 0:
+    shape = t.shape
+    if not shape:
         raise ValueError(f"{name} must have at least one axis")
-    cols = t.shape[-1]
+    cols = shape[-1]
     if t.is_contiguous():
         return (t.numel() // cols if cols else 0), cols, cols
-    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= cols:
-        return t.shape[0], cols, t.stride(0)
+    if len(shape) == 2 and t.stride(1) == 1 and t.stride(0) >= cols:
+        return shape[0], cols, t.stride(0)
     raise ValueError(f"{name} must be contiguous, or two-dimensional with contiguous rows")
 
 
@@ -834,6 +838,16 @@ def _group_rows(r: GroupRows, name: str, like: torch.Tensor) -> int:
     if group not in (32, 64, 128) or bits not in (4, 8) or cols < 0:
         raise ValueError(f"{name}: groups of 32, 64 or 128 values of 4 or 8 bits")
     words, groups = -(-cols * bits // 32), -(-cols // group)
+    at = like.get_device()
+    # one condition for what is right, for calls that last some microseconds; then what is wrong
+    if (at >= 0 and q.dtype is torch.int32 and scale.dtype is torch.float32 and q.get_device() == at
+            and scale.get_device() == at and q.is_contiguous() and scale.is_contiguous() and words and q.shape
+            and q.shape[-1] == words):
+        rows = q.numel() // words
+        n = rows * groups
+        if scale.numel() == n and (zero is None or (zero.dtype is torch.uint8 and zero.get_device() == at
+                                                    and zero.is_contiguous() and zero.numel() == n)):
+            return rows
     _dev(q, torch.int32, f"{name}.q")
     _dev(scale, torch.float32, f"{name}.scale")
     if q.dim() == 0 or q.shape[-1] != words:
@@ -845,7 +859,6 @@ def _group_rows(r: GroupRows, name: str, like: torch.Tensor) -> int:
         _dev(zero, torch.uint8, f"{name}.zero")
         if zero.numel() != rows * groups:
             raise ValueError(f"{name}.zero must hold {rows} x {groups} values")
-    at = like.get_device()
     if q.get_device() != at or scale.get_device() != at or (zero is not None and zero.get_device() != at):
         raise ValueError(f"{name} must be on the device of the other operands")
     return rows
@@ -858,7 +871,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def _out_matrix(out: Optional[torch.Tensor], shape, like: torch.Tensor, name: str = "out") -> Tuple[torch.Tensor, int]:
     """The result tensor and its row stride."""
     if out is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device), shape[-1]
+        return like.new_empty(shape), shape[-1]
     rows, cols, ld = _matrix(out, name, like)
     want = 1
     for n in shape[:-1]:

@@ -22,24 +22,27 @@ void with_type(int type, F &&f) {
     else f(bf16_t{});
 }
 
-// Every row of a float matrix starts on 16 bytes.
-inline bool rows16(const void *p, int type, int64_t ld) {
-    return ((uintptr_t)p & 15) == 0 && (ld * (type == SAMD_F32 ? 4 : 2)) % 16 == 0;
-}
-
-// n (at most 8) consecutive values as floats, 0 behind them; `vec`: p is on 16 bytes.
+// 16 bytes at the alignment of an element: global memory takes them in one access all the same.
 template <class X>
-__device__ __forceinline__ void load8(const X *p, int n, bool vec, float (&v)[8]) {
-    if (vec && n >= 8) {
-        X t[8];
-        if constexpr (sizeof(X) == 4) {
-            *(u32x4 *)t = *(const u32x4 *)p;
-            *(u32x4 *)(t + 4) = *(const u32x4 *)(p + 4);
-        } else {
-            *(u32x4 *)t = *(const u32x4 *)p;
-        }
+struct alignas(X) Bytes16 {
+    X v[16 / sizeof(X)];
+};
+template <class X>
+struct alignas(X) Four {
+    X v[4];
+};
+
+// n (at most 8) consecutive values as floats, 0 behind them.
+template <class X>
+__device__ __forceinline__ void load8(const X *p, int n, float (&v)[8]) {
+    if (n >= 8) {
+        constexpr int kHalf = 16 / sizeof(X);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+        for (int h = 0; h < 8 / kHalf; ++h) {
+            const Bytes16<X> t = *(const Bytes16<X> *)(p + h * kHalf);
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) v[h * kHalf + i] = (float)t.v[i];
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
@@ -47,16 +50,15 @@ __device__ __forceinline__ void load8(const X *p, int n, bool vec, float (&v)[8]
 }
 
 template <class X>
-__device__ __forceinline__ void store8(X *p, int n, bool vec, const float (&v)[8]) {
-    if (vec && n >= 8) {
-        X t[8];
+__device__ __forceinline__ void store8(X *p, int n, const float (&v)[8]) {
+    if (n >= 8) {
+        constexpr int kHalf = 16 / sizeof(X);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = (X)v[i];
-        if constexpr (sizeof(X) == 4) {
-            *(u32x4 *)p = *(u32x4 *)t;
-            *(u32x4 *)(p + 4) = *(u32x4 *)(t + 4);
-        } else {
-            *(u32x4 *)p = *(u32x4 *)t;
+        for (int h = 0; h < 8 / kHalf; ++h) {
+            Bytes16<X> t;
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) t.v[i] = (X)v[h * kHalf + i];
+            *(Bytes16<X> *)(p + h * kHalf) = t;
         }
     } else {
 #pragma unroll
@@ -143,10 +145,18 @@ struct Raw8 {
 
 template <class X>
 __device__ __forceinline__ Raw8<X> raw8(const X *p, int n) {   // any alignment, n of them in the row
-    X h[8];
+    Raw8<X> r;
+    if (n >= 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = i < n ? p[i] : (X)0.0f;
-    return __builtin_bit_cast(Raw8<X>, h);
+        for (int h = 0; h < (int)sizeof(X) / 2; ++h)
+            r.v[h] = __builtin_bit_cast(u32x4, *(const Bytes16<X> *)(p + h * (16 / sizeof(X))));
+    } else {
+        X h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = i < n ? p[i] : (X)0.0f;
+        r = __builtin_bit_cast(Raw8<X>, h);
+    }
+    return r;
 }
 
 // Zeroes behind the first n.

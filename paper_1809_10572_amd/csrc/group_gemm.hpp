@@ -99,13 +99,12 @@ struct TokenTile {
 
 // 4 neighbouring results of a row, `n` of them in range.
 template <class X>
-__device__ __forceinline__ void store4(X *p, int n, bool vec, const float (&v)[4]) {
-    if (vec && n >= 4) {
-        X t[4];
+__device__ __forceinline__ void store4(X *p, int n, const float (&v)[4]) {
+    if (n >= 4) {
+        Four<X> t;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = (X)v[i];
-        if constexpr (sizeof(X) == 4) *(u32x4 *)p = *(u32x4 *)t;
-        else *(u32x2 *)p = *(u32x2 *)t;
+        for (int i = 0; i < 4; ++i) t.v[i] = (X)v[i];
+        *(Four<X> *)p = t;
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -113,15 +112,8 @@ __device__ __forceinline__ void store4(X *p, int n, bool vec, const float (&v)[4
     }
 }
 
-// Every group of 4 columns of a row is on 4 elements.
-inline bool rows4(const void *p, int type, int64_t ld) {
-    const int64_t bytes = type == SAMD_F32 ? 16 : 8;
-    return (uintptr_t)p % bytes == 0 && ld % 4 == 0;
-}
-
 template <class X, bool BUF, int PER, int NW, int WT, int WM, int TW, int MW, int KS>
-__global__ __launch_bounds__(64 * TW * MW * KS) void group_gemm_kernel(GroupProduct p, int words, int groups, int tblocks,
-                                                                  bool vecy) {
+__global__ __launch_bounds__(64 * TW * MW * KS) void group_gemm_kernel(GroupProduct p, int words, int groups, int tblocks) {
     using H = std::conditional_t<std::is_same_v<X, half_t>, half_t, bf16_t>;
     constexpr int P = kPieces<X>, THREADS = 64 * TW * MW;
     constexpr int BT = 16 * WT * TW, BM = 16 * WM * MW;      // tokens and rows of W of a workgroup
@@ -325,7 +317,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_gemm_kernel(GroupProd
             for (int i = 0; i < WM; ++i) {
                 const int64_t m = m0 + (mw * WM + i) * 16 + quarter * 4;
                 const float v[4] = {acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]};
-                if (in) store4(y + m, (int)min((int64_t)4, p.M - m), vecy, v);
+                if (in) store4(y + m, (int)min((int64_t)4, p.M - m), v);
             }
         } else {
             static_assert(NW == 1 || WM == 4, "a wave's rows of each matrix are one stored group");
@@ -340,7 +332,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_gemm_kernel(GroupProd
                     activation(p.act, acc[i][t][r], v[r], da);
                     v[r] *= acc[i + WM / 2][t][r];
                 }
-                if (in) store4(y + m, (int)min((int64_t)4, p.M - m), vecy, v);
+                if (in) store4(y + m, (int)min((int64_t)4, p.M - m), v);
             }
             if (p.g8) {
                 const int64_t saved_words = ((int64_t)p.M + 3) / 4, saved_groups = ((int64_t)p.M + SAMD_GATED_GROUP - 1) / SAMD_GATED_GROUP;
@@ -381,10 +373,9 @@ int launch_gemm_tile(const GroupProduct &p, int words, int groups, hipStream_t s
         set_error("group product: T x M needs too many workgroups");
         return SAMD_EUNSUPPORTED;
     }
-    const bool vecy = rows4(p.y, p.type, p.ldy);
     auto go = [&](auto per) {
         hipLaunchKernelGGL((group_gemm_kernel<X, BUF, decltype(per)::value, NW, WT, WM, TW, MW, KS>), dim3((uint32_t)blocks),
-                           dim3(64 * TW * MW * KS), 0, s, p, words, groups, (int)tblocks, vecy);
+                           dim3(64 * TW * MW * KS), 0, s, p, words, groups, (int)tblocks);
     };
     if (p.group == 32) go(std::integral_constant<int, 1>{});
     else if (p.group == 64) go(std::integral_constant<int, 2>{});

@@ -68,7 +68,7 @@ __device__ __forceinline__ void grad_operand(const Raw8<X> &raw, u32x4 (&out)[kG
 
 template <class X, bool SIGNED, bool BUF, int WT, int WM, int TW, int MW, int KS>
 __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad p, int words, int groups, int gshift,
-                                                                       int tblocks, bool vecx) {
+                                                                       int tblocks) {
     constexpr int P = kGradPieces<X>, THREADS = 64 * TW * MW;
     constexpr int BT = 16 * WT * TW, BN = 16 * WM * MW;
     constexpr int KPT = BN * 8 / THREADS;   // columns of a thread: a half or a quarter of a word
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
         for (int i = 0; i < WM; ++i) {
             const int64_t k = k0 + (mw * WM + i) * 16 + quarter * 4;
             const float v[4] = {acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]};
-            if (token < p.T) store4((X *)p.dx + token * p.lddx + k, (int)min((int64_t)4, p.K - k), vecx, v);
+            if (token < p.T) store4((X *)p.dx + token * p.lddx + k, (int)min((int64_t)4, p.K - k), v);
         }
     }
 }
@@ -269,8 +269,7 @@ int launch_grad_tile(const GroupGrad &p, hipStream_t s) {
         return SAMD_EUNSUPPORTED;
     }
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * TW * MW * KS), 0, s, p, words, groups, gshift, (int)tblocks,
-                           rows4(p.dx, p.type, p.lddx));
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * TW * MW * KS), 0, s, p, words, groups, gshift, (int)tblocks);
     };
     p.w[0].zero ? go(group_grad_kernel<X, false, BUF, WT, WM, TW, MW, KS>) : go(group_grad_kernel<X, true, BUF, WT, WM, TW, MW, KS>);
     return check_launch("samd_group_matmul_grad");

@@ -14,24 +14,31 @@ int launch_product(const GroupProduct &p, int words, int groups, hipStream_t s) 
                     : launch_vector<X, true, NW>(p, words, groups, gshift, s);
         return check_launch("group product");
     }
-    if (p.T <= 32 && !p.g8)
+    if (p.T <= 16 && !p.g8)
         return p.w[0].zero ? launch_narrow<X, false, NW>(p, words, groups, s) : launch_narrow<X, true, NW>(p, words, groups, s);
-    // More tokens: tiles through LDS.  A workgroup fills a CU, so a tile costs its time for each round of 256
-    // workgroups; the units are microseconds measured for K = 4096, groups of 128 (they grow with K alike).
-    constexpr int kSlices = sizeof(X) == 4 ? 2 : 4;
-    if (!within_buffer(p.x, sizeof(X), std::min<int64_t>(p.T, 256), p.ldx, p.K))
-        return launch_gemm_tile<X, false, NW, 2, 4, 2, 1, kSlices>(p, words, groups, s);
+    // More tokens.  A workgroup fills a CU, so a kernel costs its time for each round of 256 workgroups; the units are
+    // microseconds measured for K = 4096, groups of 128 (they grow with K alike).
     auto cost = [&](int64_t tokens, int64_t rows, int64_t unit) {
-        const int64_t blocks = ((p.T + tokens - 1) / tokens) * ((p.M + rows / NW - 1) / (rows / NW));
+        const int64_t blocks = ((p.T + tokens - 1) / tokens) * ((p.M + rows - 1) / rows);
         return (blocks + 255) / 256 * unit;
     };
-    if constexpr (sizeof(X) == 2) {
-        const int64_t small = cost(64, 64, 23), middle = cost(128, 128, 53), large = cost(256, 128, 80);
-        if (large < middle && large < small) return launch_gemm_tile<X, true, NW, 4, 4, 4, 2, 1>(p, words, groups, s);
+    constexpr bool kWide = sizeof(X) == 4;
+    constexpr int kSlices = kWide ? 2 : 4;
+    const bool buffered = within_buffer(p.x, sizeof(X), std::min<int64_t>(p.T, 256), p.ldx, p.K);
+    int64_t narrow = p.g8 ? INT64_MAX / 2 : cost(32, 16, (kWide ? 23 : 11) + (NW > 1 ? (kWide ? 12 : 6) : 0));
+    if (!buffered) narrow *= 2;   // rows of x at odd addresses: 100 x 2001 x 1501 takes it 22 us, a tile 16
+    const int64_t small = cost(64, 64 / NW, kWide ? 55 : 23);
+    const int64_t middle = kWide ? cost(64, 128 / NW, 84) : cost(128, 128 / NW, 53);
+    const int64_t large = kWide ? cost(128, 128 / NW, 108) : cost(256, 128 / NW, 80);
+    if (narrow < std::min(small, std::min(middle, large)))
+        return p.w[0].zero ? launch_narrow<X, false, NW>(p, words, groups, s) : launch_narrow<X, true, NW>(p, words, groups, s);
+    if (!buffered)
+        return launch_gemm_tile<X, false, NW, 2, 4, 2, 1, kSlices>(p, words, groups, s);
+    if constexpr (!kWide) {
+        if (large < std::min(small, middle)) return launch_gemm_tile<X, true, NW, 4, 4, 4, 2, 1>(p, words, groups, s);
         if (middle < small) return launch_gemm_tile<X, true, NW, 4, 4, 2, 2, 2>(p, words, groups, s);
     } else {
-        const int64_t small = cost(64, 64, 55), middle = cost(64, 128, 84), large = cost(128, 128, 108);
-        if (large < middle && large < small) return launch_gemm_tile<X, true, NW, 2, 4, 4, 2, 1>(p, words, groups, s);
+        if (large < std::min(small, middle)) return launch_gemm_tile<X, true, NW, 2, 4, 4, 2, 1>(p, words, groups, s);
         if (middle < small) return launch_gemm_tile<X, true, NW, 2, 4, 2, 2, 1>(p, words, groups, s);
     }
     return launch_gemm_tile<X, true, NW, 2, 4, 2, 1, kSlices>(p, words, groups, s);

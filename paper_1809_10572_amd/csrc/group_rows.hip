@@ -16,7 +16,7 @@ constexpr int kBlock = 256;
 
 template <class X, int B, bool SIGNED>
 __global__ __launch_bounds__(kBlock) void group_quantize_kernel(const X *__restrict__ src, int64_t items, int32_t cols,
-                                                                int64_t ld, int lanes, int words, RowOf div, bool vec,
+                                                                int64_t ld, int lanes, int words, RowOf div,
                                                                 uint32_t *__restrict__ q, float *__restrict__ scale,
                                                                 uint8_t *__restrict__ zero) {
     constexpr int kTop = SIGNED ? (1 << (B - 1)) - 1 : (1 << B) - 1;
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(kBlock) void group_quantize_kernel(const X *__restr
         const int64_t k0 = (int64_t)at * 8;
         const int n = (int)min((int64_t)8, max((int64_t)0, cols - k0));
         float v[8];
-        load8(src + r * ld + k0, n, vec, v);
+        load8(src + r * ld + k0, n, v);
         uint32_t big = 0;
         float lo = 0.0f, hi = 0.0f;
 #pragma unroll
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kBlock) void group_dequantize_kernel(const uint32_t
                                                                   const float *__restrict__ scale,
                                                                   const uint8_t *__restrict__ zero, int64_t items,
                                                                   int32_t cols, int words, int groups, int gshift,
-                                                                  RowOf div, X *__restrict__ dst, int64_t ld, bool vec,
+                                                                  RowOf div, X *__restrict__ dst, int64_t ld,
                                                                   bool vecq) {
     for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < items; i += (int64_t)gridDim.x * kBlock) {
         const int64_t r = row_index(div, i);
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kBlock) void group_dequantize_kernel(const uint32_t
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = s * field_value<B, SIGNED>(f[j], z);
-        store8(dst + r * ld + k0, n, vec, v);
+        store8(dst + r * ld + k0, n, v);
     }
 }
 
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kBlock) void group_gated_grad_kernel(const X *__res
                                                                   GroupW u, int64_t items, int32_t M, int words,
                                                                   int groups, int gshift, RowOf div,
                                                                   X *__restrict__ dg, X *__restrict__ du, int64_t ldd,
-                                                                  int act, bool vech, bool vecd, bool vecq) {
+                                                                  int act, bool vecq) {
     for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < items; i += (int64_t)gridDim.x * kBlock) {
         const int64_t r = row_index(div, i);
         const int64_t at = i - r * div.per, k0 = at * 8;
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kBlock) void group_gated_grad_kernel(const X *__res
         load_fields<8>(u.q + r * words, at, n, vecq, fu);
         const float sg = g.scale[s], su = u.scale[s];
         float d[8], a[8], b[8];
-        load8(dh + r * lddh + k0, n, vech, d);
+        load8(dh + r * lddh + k0, n, d);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float value, slope;
@@ -153,8 +153,8 @@ __global__ __launch_bounds__(kBlock) void group_gated_grad_kernel(const X *__res
             a[j] = d[j] * (su * field_value<8, true>(fu[j], 0)) * slope;
             b[j] = d[j] * value;
         }
-        store8(dg + r * ldd + k0, n, vecd, a);
-        store8(du + r * ldd + k0, n, vecd, b);
+        store8(dg + r * ldd + k0, n, a);
+        store8(du + r * ldd + k0, n, b);
     }
 }
 
@@ -170,12 +170,11 @@ int launch_group_quantize(const void *src, int type, int64_t rows, int64_t cols,
     const int grid = grid_for(items, kBlock);
     const int words = (int)row_words(cols, f.bits);
     const RowOf div = row_of(items, (uint32_t)(groups * lanes));
-    const bool vec = rows16(src, type, ld);
     with_type(type, [&](auto t) {
         using X = decltype(t);
         auto go = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), 0, s, (const X *)src, items, (int32_t)cols, ld, lanes,
-                               words, div, vec, q, scale, zero);
+                               words, div, q, scale, zero);
         };
         if (f.bits == 4) f.is_signed ? go(group_quantize_kernel<X, 4, true>) : go(group_quantize_kernel<X, 4, false>);
         else f.is_signed ? go(group_quantize_kernel<X, 8, true>) : go(group_quantize_kernel<X, 8, false>);
@@ -190,12 +189,12 @@ int launch_group_dequantize(const GroupW &w, int64_t rows, int64_t cols, samd_fm
     const int grid = grid_for(items, kBlock);
     const int words = (int)row_words(cols, f.bits);
     const RowOf div = row_of(items, (uint32_t)per);
-    const bool vec = rows16(dst, type, ld), vecq = words % 2 == 0 && ((uintptr_t)w.q & 7) == 0;
+    const bool vecq = words % 2 == 0 && ((uintptr_t)w.q & 7) == 0;
     with_type(type, [&](auto t) {
         using X = decltype(t);
         auto go = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3(grid), dim3(kBlock), 0, s, w.q, w.scale, w.zero, items, (int32_t)cols,
-                               words, (int)groups, group_shift(group), div, (X *)dst, ld, vec, vecq);
+                               words, (int)groups, group_shift(group), div, (X *)dst, ld, vecq);
         };
         if (f.bits == 4)
             f.is_signed ? go(group_dequantize_kernel<X, 4, true>) : go(group_dequantize_kernel<X, 4, false>);
@@ -212,13 +211,11 @@ int launch_group_gated_grad(const void *dh, int type, int64_t lddh, const GroupW
     const int grid = grid_for(items, kBlock);
     const int words = (int)row_words(M, 8);
     const RowOf div = row_of(items, (uint32_t)per);
-    const bool vech = rows16(dh, type, lddh), vecd = rows16(dg, type, ldd) && rows16(du, type, ldd);
     const bool vecq = words % 2 == 0 && (((uintptr_t)g.q | (uintptr_t)u.q) & 7) == 0;
     with_type(type, [&](auto t) {
         using X = decltype(t);
         hipLaunchKernelGGL((group_gated_grad_kernel<X>), dim3(grid), dim3(kBlock), 0, s, (const X *)dh, lddh, g, u, items,
-                           (int32_t)M, words, (int)groups, group_shift(group), div, (X *)dg, (X *)du, ldd, act, vech, vecd,
-                           vecq);
+                           (int32_t)M, words, (int)groups, group_shift(group), div, (X *)dg, (X *)du, ldd, act, vecq);
     });
     return check_launch("samd_group_gated_grad");
 }

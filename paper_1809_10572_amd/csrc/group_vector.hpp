@@ -68,7 +68,7 @@ __device__ __forceinline__ uint32_t field_pair(uint32_t w, uint32_t one) {
 
 template <class X, bool SIGNED, int T, int NW, int R>
 __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProduct p, int words, int groups, int gshift,
-                                                                      int steps, int held, bool vecx) {
+                                                                      int steps, int held) {
     constexpr bool kWide = sizeof(X) == 4;
     constexpr int kParts = kWide ? 8 : 4;          // 16-byte parts of a lane's 32 values of x
     extern __shared__ u32x4 xs[];                  // [T][held][kParts][64], then float sums [T][held][64]
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
             const int t = i / (here * 256), j = i - t * (here * 256);   // the 8 values of word j
             const int64_t k0 = ((int64_t)s0 * 256 + j) * 8;
             float v[8] = {};
-            if (t < p.T && k0 < p.K) load8((const X *)p.x + (int64_t)t * p.ldx + k0, (int)min((int64_t)8, p.K - k0), vecx, v);
+            if (t < p.T && k0 < p.K) load8((const X *)p.x + (int64_t)t * p.ldx + k0, (int)min((int64_t)8, p.K - k0), v);
             const int at = t * held + (j >> 8), to_lane = (j & 255) >> 2;
             u32x4 *to = xs + (at * kParts + (j & 3) * (kParts / 4)) * 64 + to_lane;
             if constexpr (kWide) {   // fields come out of a word as 0, 2, 4, 6 and 1, 3, 5, 7
@@ -217,15 +217,13 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
 template <class X, bool SIGNED, int NW>
 void launch_vector(const GroupProduct &p, int words, int groups, int gshift, hipStream_t s) {
     const int steps = (words + 255) / 256;
-    const bool vecx = rows16(p.x, p.type, p.ldx);
     const bool one = p.M <= 2048;
     const int rows = kVecWaves * (one ? 1 : 2);
     const dim3 grid((uint32_t)(((int64_t)p.M + rows - 1) / rows));
     auto go = [&](auto kernel, int tokens) {
         const int step_bytes = tokens * (kVecStep * (int)sizeof(X) + 256);
         const int held = std::min(steps, std::max(2, kVecLds / step_bytes & ~1));
-        hipLaunchKernelGGL(kernel, grid, dim3(64 * kVecWaves), held * step_bytes, s, p, words, groups, gshift, steps, held,
-                           vecx);
+        hipLaunchKernelGGL(kernel, grid, dim3(64 * kVecWaves), held * step_bytes, s, p, words, groups, gshift, steps, held);
     };
     if (p.T == 1) one ? go(group_vector_kernel<X, SIGNED, 1, NW, 1>, 1) : go(group_vector_kernel<X, SIGNED, 1, NW, 2>, 1);
     else if (p.T == 2) one ? go(group_vector_kernel<X, SIGNED, 2, NW, 1>, 2) : go(group_vector_kernel<X, SIGNED, 2, NW, 2>, 2);

@@ -257,3 +257,23 @@ def test_binding_marshals_what_it_is_given(fake):
     r = samd.group_quantize(x, 8, False, 64)
     assert r.q.shape == (2, 4, 18) and r.zero.shape == r.scale.shape == (2, 4, 2) and rec.calls.pop()[1][2:5] == (8, 70, 70)
     assert samd.group_dequantize(r, torch.float16).shape == x.shape
+
+
+# ---- the compiled kernels -------------------------------------------------------------------------
+
+def test_kernels_use_no_scratch():
+    """Every kernel on group-scaled rows keeps its arrays in registers (a lambda that the compiler does not
+    inline puts them into scratch memory, which costs a product a hundredfold)."""
+    import re
+
+    from test_kernel_resources import _code_objects, _kernels
+    samd.lib()
+    with open(samd.LIB_PATH, "rb") as f:
+        blob = f.read()
+    seen = 0
+    for k in (k for elf in _code_objects(blob) for k in _kernels(elf)):
+        if not re.search(r"group_(quantize|dequantize|gated_grad|vector|narrow|gemm|grad)_kernel", k[".name"]):
+            continue
+        seen += 1
+        assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, k[".name"]
+    assert seen > 100
