@@ -297,7 +297,9 @@ int launch_grad_of(const GroupGrad &p, hipStream_t s) {
         if (cost(128, 128, 117) < cost(64, 64, 54)) return launch_grad_tile<X, true, 2, 4, 4, 2, 1>(p, s);
         return launch_grad_tile<X, true, 2, 4, 2, 1, 2>(p, s);
     } else {
-        return buffered ? launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s) : launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
+        if (!buffered) return launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
+        if (cost(64, 64, 94) < cost(32, 64, 61)) return launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s);
+        return launch_grad_tile<X, true, 2, 2, 1, 2, 2>(p, s);
     }
 }
 

@@ -2,9 +2,10 @@
 //
 // The weights still come from memory once, so they go straight into the registers that the
 // 16 x 16 x 32 matrix instruction reads: lane l holds row l % 16 of W, quarter l / 16 of the values that one
-// instruction sums over.  A step is 128 values of a row; which of them an instruction takes is free as long
-// as both operands agree and all lie in one group, so a lane's words are consecutive: PER = group / 32 words
-// for PER instructions.  As in the products of few tokens a field becomes the 16-bit float (16 + u) / 16
+// instruction sums over.  A step is 128 values of a row, 16 words, four neighbouring ones to a lane; which of them an
+// instruction takes is free as long as both operands agree and all lie in one group, so groups of 128 need no
+// exchange, groups of 64 and 32 one or two exchanges between halves and rows of lanes (PER = group / 32 instructions
+// a group).  As in the products of few tokens a field becomes the 16-bit float (16 + u) / 16
 // by half an operation, and an instruction on an operand of ones gives each token's sum of x:
 //   y += 16 s (sum x (16 + u)/16 - (1 + z/16) sum x)     once a group, in 32-bit floats.
 // 32-bit activations enter as three bf16 pieces of 8 bits each, which hold all 24 bits: the products stay
@@ -20,9 +21,22 @@ namespace samd {
 
 constexpr int kNarrowWaves = 8;
 
+// The upper 32 lanes of w[A] and the lower 32 of w[B] change places; within each half, the upper 16 lanes of w[A] and the
+// lower 16 of w[B].
+template <int A, int B>
+__device__ __forceinline__ void swap_halves(u32x4 &w) {
+    const auto r = __builtin_amdgcn_permlane32_swap(w[A], w[B], false, false);
+    w[A] = r[0], w[B] = r[1];
+}
+template <int A, int B>
+__device__ __forceinline__ void swap_rows(u32x4 &w) {
+    const auto r = __builtin_amdgcn_permlane16_swap(w[A], w[B], false, false);
+    w[A] = r[0], w[B] = r[1];
+}
+
 template <class X, bool SIGNED, int PER, int TT, int NW>
 __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupProduct p, int words, int groups,
-                                                                         bool buffered) {
+                                                                         bool buffered, bool whole_zeros) {
     constexpr int kGroups = 4 / PER;   // groups of a step
     constexpr int kTokens = 16 * TT, kRows = 16;
     using H = std::conditional_t<std::is_same_v<X, half_t>, half_t, bf16_t>;
@@ -48,13 +62,27 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
     }
     const uint32_t qrow = (uint32_t)min(low, rows - 1) * (uint32_t)words, srow = (uint32_t)min(low, rows - 1) * (uint32_t)groups;
     struct Step {
-        uint32_t w[NW][4];
+        u32x4 w[NW];
         float s[NW][kGroups];
-        uint32_t z[NW][kGroups];
+        uint32_t z[NW];   // a byte for each group
         Raw8<X> x[TT][4];
     };
-    // the 8 values of a row of x that instruction i of a step takes in this lane
-    auto k_of = [&](int step, int i) { return step * 128 + (i / PER) * 32 * PER + quarter * 8 * PER + (i % PER) * 8; };
+    // the 8 values of a row of x that instruction i of a step takes in this lane (i / PER is the group)
+    auto k_of = [&](int step, int i) {
+        const int word = PER == 4 ? quarter * 4 + i : PER == 2 ? i / 2 * 8 + quarter % 2 * 4 + quarter / 2 * 2 + i % 2 : i * 4 + quarter;
+        return step * 128 + word * 8;
+    };
+    // A lane's four neighbouring words to those of instructions 0 .. 3.
+    auto by_instruction = [](u32x4 &w) {
+        if constexpr (PER <= 2) {
+            swap_halves<0, 2>(w);
+            swap_halves<1, 3>(w);
+        }
+        if constexpr (PER == 1) {
+            swap_rows<0, 1>(w);
+            swap_rows<2, 3>(w);
+        }
+    };
 
     f32x4 acc[NW][TT] = {};
     // BUF: rows of x on 4 bytes, within 4 GB of each other: read through one descriptor, any 4-byte alignment
@@ -75,24 +103,28 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
             }
         };
         auto fetch = [&](int step, Step &f) {
+            const uint32_t g = srow + (uint32_t)(min(step, steps - 1) * kGroups);
+            if constexpr (!SIGNED) {   // first, so that waits for what follows count the same either way
 #pragma unroll
-            for (int a = 0; a < NW; ++a) {
-#pragma unroll
-                for (int c = 0; c < kGroups; ++c) {
-                    const uint32_t at = step < steps ? (qrow + step * 16 + c * 4 * PER + quarter * PER) * 4 : 0xffffff00u;
-                    if constexpr (PER == 4) {
-                        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rq[a], at, 0, 0);
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) f.w[a][b] = v[b];
-                    } else if constexpr (PER == 2) {
-                        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rq[a], at, 0, 0);
-                        f.w[a][c * 2] = v[0], f.w[a][c * 2 + 1] = v[1];
+                for (int a = 0; a < NW; ++a) {
+                    if (kGroups == 1) {
+                        f.z[a] = __builtin_amdgcn_raw_buffer_load_b8(rz[a], g, 0, 0);
+                    } else if (whole_zeros) {
+                        f.z[a] = kGroups == 4 ? __builtin_amdgcn_raw_buffer_load_b32(rz[a], g, 0, 0)
+                                              : __builtin_amdgcn_raw_buffer_load_b16(rz[a], g, 0, 0);
                     } else {
-                        f.w[a][c] = __builtin_amdgcn_raw_buffer_load_b32(rq[a], at, 0, 0);
+                        f.z[a] = 0;
+#pragma unroll
+                        for (int c = 0; c < kGroups; ++c)
+                            f.z[a] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rz[a], g + c, 0, 0) << (8 * c);
                     }
                 }
+            }
+#pragma unroll
+            for (int a = 0; a < NW; ++a) {
+                const uint32_t at = step < steps ? (qrow + step * 16 + quarter * 4) * 4 : 0xffffff00u;
+                f.w[a] = __builtin_amdgcn_raw_buffer_load_b128(rq[a], at, 0, 0);
                 // a step's scales together; those behind the row's last group are not used below
-                const uint32_t g = srow + (uint32_t)min(step * kGroups, groups - 1);
                 if constexpr (kGroups == 4) {
                     const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs[a], g * 4, 0, 0);
 #pragma unroll
@@ -103,9 +135,6 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                 } else {
                     f.s[a][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs[a], g * 4, 0, 0));
                 }
-                if (!SIGNED)
-#pragma unroll
-                    for (int c = 0; c < kGroups; ++c) f.z[a][c] = __builtin_amdgcn_raw_buffer_load_b8(rz[a], g + c, 0, 0);
             }
 #pragma unroll
             for (int t = 0; t < TT; ++t)
@@ -113,6 +142,9 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                 for (int i = 0; i < 4; ++i) f.x[t][i] = x_at(t, step, i);
         };
         auto use = [&](const Step &f, int step) {
+            u32x4 words_of[NW];
+#pragma unroll
+            for (int a = 0; a < NW; ++a) by_instruction(words_of[a] = f.w[a]);
 #pragma unroll
             for (int c = 0; c < kGroups; ++c) {
                 f32x4 part[NW][TT] = {}, sum[TT] = {};
@@ -133,7 +165,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                         for (int j = 0; j < kPieces<X>; ++j) sum[t] = mfma<H>(x[t][j], ones, sum[t]);
 #pragma unroll
                     for (int a = 0; a < NW; ++a) {
-                        const uint32_t w = f.w[a][i];
+                        const uint32_t w = words_of[a][i];
                         const u32x4 v = {field_pair<H, 0>(w, kField), field_pair<H, 1>(w, kField), field_pair<H, 2>(w, kField),
                                          field_pair<H, 3>(w, kField)};
 #pragma unroll
@@ -145,7 +177,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                 if (kGroups > 1 && step * kGroups + c >= groups) break;   // behind the row's last group
 #pragma unroll
                 for (int a = 0; a < NW; ++a) {
-                    const float z = SIGNED ? 8.0f : (float)f.z[a][c];
+                    const float z = SIGNED ? 8.0f : (float)((f.z[a] >> (8 * c)) & 255u);
                     const float zz = fmaf(z, -0.0625f, -1.0f), s = 16.0f * f.s[a][c];
 #pragma unroll
                     for (int t = 0; t < TT; ++t)
@@ -207,8 +239,12 @@ int launch_narrow(const GroupProduct &p, int words, int groups, hipStream_t s) {
         return SAMD_EUNSUPPORTED;
     }
     const bool buffered = within_buffer(p.x, sizeof(X), std::min<int64_t>(p.T, 32), p.ldx, p.K);
+    // a step's zero points (4 bytes for groups of 32, 2 for groups of 64) in one access
+    bool whole_zeros = groups % (128 / p.group) == 0;
+    for (int a = 0; a < NW; ++a) whole_zeros = whole_zeros && (uintptr_t)p.w[a].zero % (128 / p.group) == 0;
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * kNarrowWaves), 0, s, p, words, groups, buffered);
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * kNarrowWaves), 0, s, p, words, groups, buffered,
+                           whole_zeros);
     };
     auto with_group = [&](auto per) {
         constexpr int PER = decltype(per)::value;
