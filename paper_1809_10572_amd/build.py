@@ -22,7 +22,7 @@ SOURCES = ["api.cpp", "plan.cpp", "pack.hip", "conv1d.hip", "conv2d_multiply_row
            "conv2d_multiply_rows3_wide.hip", "conv2d_multiply_rows5.hip", "conv2d_multiply_general.hip",
            "conv2d_multiply_batches.hip", "conv2d_samd.hip",
            "conv2d_spread.hip", "conv2d_i8.hip", "epilogue.hip", "lanewise.hip", "peaks.hip", "noalloc.hip",
-           "group_rows.hip", "group_product_f32.hip", "group_product_f16.hip", "group_product_bf16.hip", "group_grad.hip"]
+           "group_rows.hip", "group_grad.hip"] + [f"group_{op}_{t}.hip" for op in ("product", "gated") for t in ("f32", "f16", "bf16")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall", "-Wno-unused-function",

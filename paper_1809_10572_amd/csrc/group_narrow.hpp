@@ -11,8 +11,11 @@
 // 32-bit activations enter as three bf16 pieces of 8 bits each, which hold all 24 bits: the products stay
 // exact, three instructions for each.
 //
-// A workgroup computes 16 rows of W for 16 TT tokens, its eight waves taking steps of K in turn; their
+// A workgroup computes 16 MT rows of W for 16 TT tokens, its eight waves taking steps of K in turn; their
 // sums meet in LDS in a fixed order.
+//
+// Bound by what each CU reads of x through L1 and by the latency of a wave's few steps: 16 x 4096 x 4096 bf16 takes 8.5 us
+// (signed groups of 128), 16 x 8192 x 8192 22 us, against 1.8 and 7 for reading the weights once at 5.2 TB/s.
 #pragma once
 
 #include "group_vector.hpp"
@@ -34,16 +37,17 @@ __device__ __forceinline__ void swap_rows(u32x4 &w) {
     w[A] = r[0], w[B] = r[1];
 }
 
-template <class X, bool SIGNED, int PER, int TT, int NW>
+template <class X, bool SIGNED, int PER, int TT, int NW, int MT>
 __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupProduct p, int words, int groups,
                                                                          bool buffered, bool whole_zeros) {
     constexpr int kGroups = 4 / PER;   // groups of a step
-    constexpr int kTokens = 16 * TT, kRows = 16;
+    constexpr int kTokens = 16 * TT, kRows = 16 * MT;
+    constexpr int NR = NW * MT;   // 16-row sets: set r is rows r % MT * 16 .. of matrix r / MT
     using H = std::conditional_t<std::is_same_v<X, half_t>, half_t, bf16_t>;
     constexpr uint32_t kOnes = std::is_same_v<H, half_t> ? 0x3c003c00u : 0x3f803f80u;
     constexpr uint32_t kField = std::is_same_v<H, half_t> ? (SIGNED ? 0x3e003e00u : 0x3c003c00u)
                                                           : (SIGNED ? 0x3fc03fc0u : 0x3f803f80u);
-    constexpr int kPart = NW * TT * 4;   // sums of a lane
+    constexpr int kPart = NR * TT * 4;   // sums of a lane
     __shared__ float meet[kNarrowWaves * kPart * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int quarter = lane >> 4, low = lane & 15;
@@ -60,11 +64,16 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
         rs[a] = buffer_of(p.w[a].scale + m0 * groups, (int64_t)rows * groups * 4);
         rz[a] = buffer_of(p.w[a].zero + m0 * groups, SIGNED ? 0 : (int64_t)rows * groups);
     }
-    const uint32_t qrow = (uint32_t)min(low, rows - 1) * (uint32_t)words, srow = (uint32_t)min(low, rows - 1) * (uint32_t)groups;
+    uint32_t qrow[MT], srow[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const uint32_t r = (uint32_t)min(m * 16 + low, rows - 1);
+        qrow[m] = r * (uint32_t)words, srow[m] = r * (uint32_t)groups;
+    }
     struct Step {
-        u32x4 w[NW];
-        float s[NW][kGroups];
-        uint32_t z[NW];   // a byte for each group
+        u32x4 w[NR];
+        float s[NR][kGroups];
+        uint32_t z[NR];   // a byte for each group
         Raw8<X> x[TT][4];
     };
     // the 8 values of a row of x that instruction i of a step takes in this lane (i / PER is the group)
@@ -84,7 +93,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
         }
     };
 
-    f32x4 acc[NW][TT] = {};
+    f32x4 acc[NR][TT] = {};
     // BUF: rows of x on 4 bytes, within 4 GB of each other: read through one descriptor, any 4-byte alignment
     auto body = [&](auto buf) {
         constexpr bool BUF = decltype(buf)::value;
@@ -103,37 +112,39 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
             }
         };
         auto fetch = [&](int step, Step &f) {
-            const uint32_t g = srow + (uint32_t)(min(step, steps - 1) * kGroups);
+            const uint32_t g0 = (uint32_t)(min(step, steps - 1) * kGroups);
             if constexpr (!SIGNED) {   // first, so that waits for what follows count the same either way
 #pragma unroll
-                for (int a = 0; a < NW; ++a) {
+                for (int a = 0; a < NR; ++a) {
+                    const uint32_t g = srow[a % MT] + g0;
                     if (kGroups == 1) {
-                        f.z[a] = __builtin_amdgcn_raw_buffer_load_b8(rz[a], g, 0, 0);
+                        f.z[a] = __builtin_amdgcn_raw_buffer_load_b8(rz[a / MT], g, 0, 0);
                     } else if (whole_zeros) {
-                        f.z[a] = kGroups == 4 ? __builtin_amdgcn_raw_buffer_load_b32(rz[a], g, 0, 0)
-                                              : __builtin_amdgcn_raw_buffer_load_b16(rz[a], g, 0, 0);
+                        f.z[a] = kGroups == 4 ? __builtin_amdgcn_raw_buffer_load_b32(rz[a / MT], g, 0, 0)
+                                              : __builtin_amdgcn_raw_buffer_load_b16(rz[a / MT], g, 0, 0);
                     } else {
                         f.z[a] = 0;
 #pragma unroll
                         for (int c = 0; c < kGroups; ++c)
-                            f.z[a] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rz[a], g + c, 0, 0) << (8 * c);
+                            f.z[a] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rz[a / MT], g + c, 0, 0) << (8 * c);
                     }
                 }
             }
 #pragma unroll
-            for (int a = 0; a < NW; ++a) {
-                const uint32_t at = step < steps ? (qrow + step * 16 + quarter * 4) * 4 : 0xffffff00u;
-                f.w[a] = __builtin_amdgcn_raw_buffer_load_b128(rq[a], at, 0, 0);
+            for (int a = 0; a < NR; ++a) {
+                const uint32_t g = srow[a % MT] + g0;
+                const uint32_t at = step < steps ? (qrow[a % MT] + step * 16 + quarter * 4) * 4 : 0xffffff00u;
+                f.w[a] = __builtin_amdgcn_raw_buffer_load_b128(rq[a / MT], at, 0, 0);
                 // a step's scales together; those behind the row's last group are not used below
                 if constexpr (kGroups == 4) {
-                    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs[a], g * 4, 0, 0);
+                    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs[a / MT], g * 4, 0, 0);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) f.s[a][c] = __uint_as_float(v[c]);
                 } else if constexpr (kGroups == 2) {
-                    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs[a], g * 4, 0, 0);
+                    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs[a / MT], g * 4, 0, 0);
                     f.s[a][0] = __uint_as_float(v[0]), f.s[a][1] = __uint_as_float(v[1]);
                 } else {
-                    f.s[a][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs[a], g * 4, 0, 0));
+                    f.s[a][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs[a / MT], g * 4, 0, 0));
                 }
             }
 #pragma unroll
@@ -142,12 +153,12 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                 for (int i = 0; i < 4; ++i) f.x[t][i] = x_at(t, step, i);
         };
         auto use = [&](const Step &f, int step) {
-            u32x4 words_of[NW];
+            u32x4 words_of[NR];
 #pragma unroll
-            for (int a = 0; a < NW; ++a) by_instruction(words_of[a] = f.w[a]);
+            for (int a = 0; a < NR; ++a) by_instruction(words_of[a] = f.w[a]);
 #pragma unroll
             for (int c = 0; c < kGroups; ++c) {
-                f32x4 part[NW][TT] = {}, sum[TT] = {};
+                f32x4 part[NR][TT] = {}, sum[TT] = {};
 #pragma unroll
                 for (int b = 0; b < PER; ++b) {
                     const int i = c * PER + b;
@@ -164,7 +175,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
 #pragma unroll
                         for (int j = 0; j < kPieces<X>; ++j) sum[t] = mfma<H>(x[t][j], ones, sum[t]);
 #pragma unroll
-                    for (int a = 0; a < NW; ++a) {
+                    for (int a = 0; a < NR; ++a) {
                         const uint32_t w = words_of[a][i];
                         const u32x4 v = {field_pair<H, 0>(w, kField), field_pair<H, 1>(w, kField), field_pair<H, 2>(w, kField),
                                          field_pair<H, 3>(w, kField)};
@@ -176,7 +187,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                 }
                 if (kGroups > 1 && step * kGroups + c >= groups) break;   // behind the row's last group
 #pragma unroll
-                for (int a = 0; a < NW; ++a) {
+                for (int a = 0; a < NR; ++a) {
                     const float z = SIGNED ? 8.0f : (float)((f.z[a] >> (8 * c)) & 255u);
                     const float zz = fmaf(z, -0.0625f, -1.0f), s = 16.0f * f.s[a][c];
 #pragma unroll
@@ -203,7 +214,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
 
     // the waves' sums meet in LDS and are added in the waves' order
 #pragma unroll
-    for (int a = 0; a < NW; ++a)
+    for (int a = 0; a < NR; ++a)
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
@@ -212,13 +223,13 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
     for (int n = threadIdx.x; n < kTokens * kRows; n += 64 * kNarrowWaves) {
         const int t = n / kRows, m = n % kRows;
         if (t >= tokens || m >= rows) continue;
-        // lane (quarter, low) held tokens 4 quarter + r of row `low`
-        const int at = (t / 16 * 4 + t % 4) * 64 + t % 16 / 4 * 16 + m;
+        // lane (quarter, low) held tokens 4 quarter + r of row `low` of a set
+        const int at = ((m / 16 * TT + t / 16) * 4 + t % 4) * 64 + t % 16 / 4 * 16 + m % 16;
         float v[NW] = {};
 #pragma unroll
         for (int a = 0; a < NW; ++a)
 #pragma unroll
-            for (int w = 0; w < kNarrowWaves; ++w) v[a] += meet[(w * kPart + a * TT * 4) * 64 + at];
+            for (int w = 0; w < kNarrowWaves; ++w) v[a] += meet[(w * kPart + a * MT * TT * 4) * 64 + at];
         float out = v[0];
         if constexpr (NW > 1) {
             float da;
@@ -229,11 +240,15 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
     }
 }
 
-// Launches the kernel: 16 tokens a workgroup, or 32.
+// Launches the kernel: 16 tokens a workgroup, or 32; 16 rows of W, or, where those are two workgroups and more for each
+// CU, 32, which read x half as often (16 x 8192 x 8192, unsigned groups of 64: 28.8 us with 16 rows, 22.0 with 32;
+// 16 x 4096 x 4096: 9.7 and 12.9).  The gated block's two matrices share x already: 32 rows of each are slower always.
 template <class X, bool SIGNED, int NW>
 int launch_narrow(const GroupProduct &p, int words, int groups, hipStream_t s) {
     const int tt = p.T <= 16 ? 1 : 2;
-    const int64_t blocks = (((int64_t)p.M + 15) / 16) * (((int64_t)p.T + 16 * tt - 1) / (16 * tt));
+    const int64_t tblocks = ((int64_t)p.T + 16 * tt - 1) / (16 * tt);
+    const int mt = NW == 1 && tblocks * (((int64_t)p.M + 15) / 16) >= 512 ? 2 : 1;
+    const int64_t blocks = tblocks * (((int64_t)p.M + 16 * mt - 1) / (16 * mt));
     if (blocks > INT32_MAX) {
         set_error("group product: T x M needs too many workgroups");
         return SAMD_EUNSUPPORTED;
@@ -248,7 +263,12 @@ int launch_narrow(const GroupProduct &p, int words, int groups, hipStream_t s) {
     };
     auto with_group = [&](auto per) {
         constexpr int PER = decltype(per)::value;
-        tt == 1 ? go(group_narrow_kernel<X, SIGNED, PER, 1, NW>) : go(group_narrow_kernel<X, SIGNED, PER, 2, NW>);
+        if constexpr (NW == 1)
+            if (mt == 2) {
+                tt == 1 ? go(group_narrow_kernel<X, SIGNED, PER, 1, NW, 2>) : go(group_narrow_kernel<X, SIGNED, PER, 2, NW, 2>);
+                return;
+            }
+        tt == 1 ? go(group_narrow_kernel<X, SIGNED, PER, 1, NW, 1>) : go(group_narrow_kernel<X, SIGNED, PER, 2, NW, 1>);
     };
     if (p.group == 32) with_group(std::integral_constant<int, 1>{});
     else if (p.group == 64) with_group(std::integral_constant<int, 2>{});

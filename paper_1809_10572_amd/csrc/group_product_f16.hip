@@ -1,10 +1,10 @@
-// Products with 4-bit group-scaled weights for f16 activations.
+// Products of f16 activations with 4-bit group-scaled weights.
 #include <hip/hip_runtime.h>
 
 #include "group_product.hpp"
 
 namespace samd {
 
-int launch_group_product_f16(const GroupProduct &p, hipStream_t s) { return launch_product_of<half_t>(p, s); }
+int launch_group_product_f16(const GroupProduct &p, hipStream_t s) { return launch_product<half_t, 1>(p, s); }
 
 }  // namespace samd

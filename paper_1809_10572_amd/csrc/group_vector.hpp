@@ -1,4 +1,4 @@
-// Products of one to four tokens with 4-bit group-scaled weights (the decoding step of a language
+// Products of one or two tokens with 4-bit group-scaled weights (the decoding step of a language
 // model): y[t][m] = sum_g s[m][g] sum_{k in g} (u[m][k] - z[m][g]) x[t][k], u the field 0..15
 // (a signed field with its sign bit flipped, its zero point then being 8).
 //
@@ -12,8 +12,7 @@
 // The offset of 16 costs the 32-bit sum two bits at most; the products themselves are exact.
 //
 // Measured (graph of calls, bf16, one token): 16384 x 8192 weights 14.8 us, 4.8 TB/s of weights, scales and x;
-// 4096 x 4096 4.6 us, of which a launch that does next to nothing (512 x 512) is 3.5.  With more tokens the
-// dot products bound it: four tokens take 8192 x 8192 through in 22 us.
+// 4096 x 4096 4.6 us, of which a launch that does next to nothing (512 x 512) is 3.5.
 //
 // A wave computes R rows of each matrix along all of K, 2048 values a step, the next step's weights
 // requested before this one's are used; x waits in LDS in the order in which fields come out of a
@@ -211,7 +210,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
         }
 }
 
-// Launches the kernel for p.T tokens (at most 4).  Two rows a wave, so that x is read from LDS half as
+// Launches the kernel for p.T tokens (1 or 2).  Two rows a wave, so that x is read from LDS half as
 // often, unless that leaves CUs without a workgroup (1024 x 16384 weights: 7.4 us with one row a wave,
 // 9.5 with two; 16384 x 8192: 17.7 and 14.8).
 template <class X, bool SIGNED, int NW>
@@ -226,8 +225,7 @@ void launch_vector(const GroupProduct &p, int words, int groups, int gshift, hip
         hipLaunchKernelGGL(kernel, grid, dim3(64 * kVecWaves), held * step_bytes, s, p, words, groups, gshift, steps, held);
     };
     if (p.T == 1) one ? go(group_vector_kernel<X, SIGNED, 1, NW, 1>, 1) : go(group_vector_kernel<X, SIGNED, 1, NW, 2>, 1);
-    else if (p.T == 2) one ? go(group_vector_kernel<X, SIGNED, 2, NW, 1>, 2) : go(group_vector_kernel<X, SIGNED, 2, NW, 2>, 2);
-    else one ? go(group_vector_kernel<X, SIGNED, 4, NW, 1>, 4) : go(group_vector_kernel<X, SIGNED, 4, NW, 2>, 4);
+    else one ? go(group_vector_kernel<X, SIGNED, 2, NW, 1>, 2) : go(group_vector_kernel<X, SIGNED, 2, NW, 2>, 2);
 }
 
 }  // namespace samd

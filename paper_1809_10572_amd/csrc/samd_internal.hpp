@@ -217,10 +217,14 @@ struct GroupProduct {
 int launch_group_product_f32(const GroupProduct &p, hipStream_t s);
 int launch_group_product_f16(const GroupProduct &p, hipStream_t s);
 int launch_group_product_bf16(const GroupProduct &p, hipStream_t s);
+int launch_group_gated_f32(const GroupProduct &p, hipStream_t s);
+int launch_group_gated_f16(const GroupProduct &p, hipStream_t s);
+int launch_group_gated_bf16(const GroupProduct &p, hipStream_t s);
 inline int launch_group_product(const GroupProduct &p, hipStream_t s) {
-    return p.type == SAMD_F32   ? launch_group_product_f32(p, s)
-           : p.type == SAMD_F16 ? launch_group_product_f16(p, s)
-                                : launch_group_product_bf16(p, s);
+    const bool one = p.act < 0;
+    if (p.type == SAMD_F32) return one ? launch_group_product_f32(p, s) : launch_group_gated_f32(p, s);
+    if (p.type == SAMD_F16) return one ? launch_group_product_f16(p, s) : launch_group_gated_f16(p, s);
+    return one ? launch_group_product_bf16(p, s) : launch_group_gated_bf16(p, s);
 }
 
 // dx = dy[0] W[0] (+ dy[1] W[1] where dy[1] is not NULL)
