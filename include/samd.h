@@ -548,8 +548,9 @@ int samd_group_dequantize(const uint32_t *q, const float *scale, const uint8_t *
                           samd_fmt f, int32_t group, void *dst, int32_t type, int64_t ld, hipStream_t stream);
 
 /* y = x W^T: x is T x K, W is M group-scaled rows of K 4-bit values (wf.bits 4), y is T x M
- * of x's type.  T = 1 is a matrix-vector product.  An x row that holds an infinity or a NaN
- * gives a y row of NaN and infinities. */
+ * of x's type.  T = 1 is a matrix-vector product.  A group's sum is taken over whole values
+ * and scaled last, so an x row that holds an infinity, a NaN or a magnitude above 2^100 may
+ * give a y row of NaN and infinities; other rows are not touched by it. */
 int samd_group_matmul(const void *x, int32_t type, int64_t ldx, const uint32_t *q, const float *scale,
                       const uint8_t *zero, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K, void *y,
                       int64_t ldy, hipStream_t stream);

@@ -2,7 +2,7 @@
 //
 // The sum runs over the rows of W, and a group's scale differs from row to row, so it is part of the summed product
 // and has to be multiplied into an operand: a weight s (u - z) is computed in 32-bit floats and enters
-//   bf16  as one bf16, rounded: an error of at most 2^-9 of each weight, as small as that of dy itself
+//   bf16  as one bf16, rounded: off by at most 2^-8 of each weight, as the types of dy and dx are
 //   f16   as two bf16 of together 16 bits and more, dy as two that hold its 11 bits: three instructions a product
 //   f32   as three bf16 of 8 bits, as is dy: the six largest of their products, off by 2^-24
 // (a bf16 holds any float's range; an f16 operand would lose small scales).  Everything is summed in 32-bit floats, both
@@ -298,7 +298,9 @@ int launch_grad_of(const GroupGrad &p, hipStream_t s) {
         return launch_grad_tile<X, true, 2, 4, 2, 1, 2>(p, s);
     } else {
         if (!buffered) return launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
-        if (cost(64, 64, 94) < cost(32, 64, 61)) return launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s);
+        const int64_t small = cost(32, 64, 61), middle = cost(64, 64, 94), large = cost(64, 128, 118);
+        if (large < middle && large < small) return launch_grad_tile<X, true, 2, 2, 2, 4, 1>(p, s);
+        if (middle < small) return launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s);
         return launch_grad_tile<X, true, 2, 2, 1, 2, 2>(p, s);
     }
 }

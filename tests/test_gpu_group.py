@@ -343,6 +343,91 @@ def tiny(typ):
     return {"f32": 2.0 ** -150, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}[typ]
 
 
+# ---- many tokens: the larger tiles ----------------------------------------------------------------
+
+def gpu_rows(gen, rows, cols, group, signed):
+    """Random 4-bit rows made and read on the GPU: (GroupRows, float64 values, float64 magnitudes)."""
+    q = torch.randint(0, 16, (rows, -(-cols // 8) * 8), generator=gen, device=DEV)
+    q[:, cols:] = 0
+    words = (q.view(rows, -1, 8) << torch.arange(0, 32, 4, device=DEV)).sum(2)
+    words = torch.where(words >= 2 ** 31, words - 2 ** 32, words).to(torch.int32)
+    groups = -(-cols // group)
+    scale = (torch.rand(rows, groups, generator=gen, device=DEV) + 0.5) / (4 * cols ** 0.5)
+    zero = None if signed else torch.randint(0, 16, (rows, groups), generator=gen, device=DEV).to(torch.uint8)
+    at = torch.arange(cols, device=DEV) // group
+    q = q[:, :cols]
+    whole = torch.where(q >= 8, q - 16, q) if signed else q - zero.long()[:, at]
+    fields = (q ^ 8) + 8 if signed else q + zero.long()[:, at]
+    s = scale.double()[:, at]
+    return GroupRows(words, scale, zero, cols, 4, group), s * whole, s * fields
+
+
+def gpu_matrix(gen, rows, cols, typ, pad):
+    t = torch.full((rows, cols + pad), float("nan"), device=DEV, dtype=TYPES[typ])[:, :cols]
+    t.copy_(torch.randn(rows, cols, generator=gen, device=DEV))
+    return t, t.double()
+
+
+def gpu_close(got, want, bound, what=""):
+    off = (got.double() - want).abs() - bound
+    fine = bool(torch.isfinite(got).all()) and float(off.max()) <= 0
+    assert fine, (what, float(off.max()))
+
+
+# tokens, rows of the result, summed values: sizes for which few tiles of 64 x 64 are not the least work, whose
+# sums run over several turns of the pipeline, with and without a ragged end, at even and odd row strides
+MANY = [(1000, 2100, 1096, 0), (1000, 2000, 1024, 8), (510, 2000, 1100, 0), (500, 2100, 1088, 2), (2040, 4090, 576, 0),
+        (2048, 4096, 330, 0), (300, 1100, 700, 3)]
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", MANY)
+def test_many_tokens(typ, size):
+    T, M, K, pad = size
+    gen = torch.Generator(device=DEV).manual_seed(T + M)
+    for group, signed in ((32, False), (64, True), (128, False)):
+        w, values, sizes = gpu_rows(gen, M, K, group, signed)
+        x, xv = gpu_matrix(gen, T, K, typ, pad)
+        want = xv @ values.t()
+        gpu_close(samd.group_matmul(x, w), want, half_step(typ) * want.abs() + depth(K) * (xv.abs() @ sizes.t()), ("y", group))
+        # the same sizes for the gradient: M summed over, K of them the result's columns
+        w, values, sizes = gpu_rows(gen, K, M, group, signed)
+        w2, values2, sizes2 = gpu_rows(gen, K, M, group, signed)
+        dy, dyv = gpu_matrix(gen, T, K, typ, pad)
+        dy2, dyv2 = gpu_matrix(gen, T, K, typ, pad)
+        rounding = {"f32": 0.0, "f16": 2.0 ** -15, "bf16": 2.0 ** -8}[typ]
+        want = dyv @ values
+        bound = rounding * (dyv.abs() @ values.abs()) + depth(K) * (dyv.abs() @ sizes)
+        gpu_close(samd.group_matmul_grad(dy, w), want, half_step(typ) * want.abs() + bound, ("dx", group))
+        want = want + dyv2 @ values2
+        bound = bound + rounding * (dyv2.abs() @ values2.abs()) + depth(2 * K) * (dyv.abs() @ sizes + dyv2.abs() @ sizes2)
+        gpu_close(samd.group_matmul_grad(dy, w, dy2, w2), want, half_step(typ) * want.abs() + bound, ("dx, two", group))
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(1000, 1050, 1096, 0), (1000, 1000, 1024, 8), (2040, 2030, 576, 0), (300, 550, 700, 3)])
+def test_gated_of_many_tokens(typ, size):
+    T, M, K, pad = size
+    gen = torch.Generator(device=DEV).manual_seed(T + M)
+    for group, signed, act in ((32, False, "silu"), (64, True, "gelu"), (128, False, "silu")):
+        wg, gv, gs = gpu_rows(gen, M, K, group, signed)
+        wu, uv, us = gpu_rows(gen, M, K, group, signed)
+        x, xv = gpu_matrix(gen, T, K, typ, pad)
+        g, u = xv @ gv.t(), xv @ uv.t()
+        dg, du = depth(K) * (xv.abs() @ gs.t()), depth(K) * (xv.abs() @ us.t())
+        a = torch.nn.functional.silu(g) if act == "silu" else torch.nn.functional.gelu(g)
+        want = a * u
+        bound = half_step(typ) * want.abs() + 1.2 * dg * (u.abs() + du) + a.abs() * du + 16 * 2.0 ** -24 * (g * u).abs()
+        gpu_close(samd.group_gated(x, wg, wu, act), want, bound, group)
+        h, g8, u8 = samd.group_gated_save(x, wg, wu, act)
+        gpu_close(h, want, bound, (group, "save"))
+        for r, v, d in ((g8, g, dg), (u8, u, du)):   # half a step of the scale and the sums' own error, also in the span
+            back = samd.group_dequantize(r)
+            step = r.scale.double().repeat_interleave(32, 1)[:, :M]
+            span = torch.nn.functional.pad(d, (0, -M % 32)).view(T, -1, 32).amax(2).repeat_interleave(32, 1)[:, :M]
+            gpu_close(back, v, 0.5 * step * (1 + 2.0 ** -20) + d + span + 2.0 ** -22 * v.abs(), (group, "stored"))
+
+
 # ---- the operators together -----------------------------------------------------------------------
 
 @pytest.mark.parametrize("typ", ["f16", "bf16", "f32"])
