@@ -22,48 +22,74 @@ void with_type(int type, F &&f) {
     else f(bf16_t{});
 }
 
-// 16 bytes at the alignment of an element: global memory takes them in one access all the same.
+// v, of which the compiler knows nothing: bytes of a masked word are converted to floats where they stand,
+// not cut out first.
+__device__ __forceinline__ uint32_t as_is(uint32_t v) {
+    asm("" : "+v"(v));
+    return v;
+}
+
+// v as a 32-bit float: a product that is stored as f16 would be rounded to it at once, not to float first as defined.
+__device__ __forceinline__ float as_float(float v) {
+    asm("" : "+v"(v));
+    return v;
+}
+
+// 16 and 8 bytes at the alignment of an element of 2 or 4: global memory takes them in one access all the same.  (As
+// words, not as elements: the compiler would take stores of the last element out of both branches below.)
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
 template <class X>
-struct alignas(X) Bytes16 {
-    X v[16 / sizeof(X)];
+using Bytes16 = std::conditional_t<sizeof(X) == 4, u32x4_at4, u32x4_at2>;
+
+// 8 values, and the same as words.
+template <class X>
+struct Eight {
+    X v[8];
 };
 template <class X>
-struct alignas(X) Four {
-    X v[4];
+struct Raw8 {
+    u32x4 v[sizeof(X) / 2];
 };
 
-// n (at most 8) consecutive values as floats, 0 behind them.
+// 8 consecutive values as they are stored, n of them in the row (at most; 0 behind them).
+template <class X>
+__device__ __forceinline__ Raw8<X> raw8(const X *p, int n) {
+    Raw8<X> r;
+    if (n >= 8) {
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(X) / 2; ++h) r.v[h] = ((const Bytes16<X> *)p)[h];
+    } else {
+        Eight<X> t;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t.v[i] = i < n ? p[i] : (X)0.0f;
+        r = __builtin_bit_cast(Raw8<X>, t);
+    }
+    return r;
+}
+
+// The same as floats.
 template <class X>
 __device__ __forceinline__ void load8(const X *p, int n, float (&v)[8]) {
-    if (n >= 8) {
-        constexpr int kHalf = 16 / sizeof(X);
+    const Eight<X> t = __builtin_bit_cast(Eight<X>, raw8(p, n));
 #pragma unroll
-        for (int h = 0; h < 8 / kHalf; ++h) {
-            const Bytes16<X> t = *(const Bytes16<X> *)(p + h * kHalf);
-#pragma unroll
-            for (int i = 0; i < kHalf; ++i) v[h * kHalf + i] = (float)t.v[i];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)t.v[i];
 }
 
 template <class X>
 __device__ __forceinline__ void store8(X *p, int n, const float (&v)[8]) {
+    Eight<X> t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.v[i] = (X)as_float(v[i]);
     if (n >= 8) {
-        constexpr int kHalf = 16 / sizeof(X);
+        const Raw8<X> w = __builtin_bit_cast(Raw8<X>, t);
 #pragma unroll
-        for (int h = 0; h < 8 / kHalf; ++h) {
-            Bytes16<X> t;
-#pragma unroll
-            for (int i = 0; i < kHalf; ++i) t.v[i] = (X)v[h * kHalf + i];
-            *(Bytes16<X> *)(p + h * kHalf) = t;
-        }
+        for (int h = 0; h < (int)sizeof(X) / 2; ++h) ((Bytes16<X> *)p)[h] = w.v[h];
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = (X)v[i];
+            if (i < n) p[i] = t.v[i];
     }
 }
 
@@ -137,28 +163,6 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
 template <class X>
 constexpr int kPieces = sizeof(X) == 4 ? 3 : 1;
 
-// 8 values of a row as they are stored.
-template <class X>
-struct Raw8 {
-    u32x4 v[sizeof(X) / 2];
-};
-
-template <class X>
-__device__ __forceinline__ Raw8<X> raw8(const X *p, int n) {   // any alignment, n of them in the row
-    Raw8<X> r;
-    if (n >= 8) {
-#pragma unroll
-        for (int h = 0; h < (int)sizeof(X) / 2; ++h)
-            r.v[h] = __builtin_bit_cast(u32x4, *(const Bytes16<X> *)(p + h * (16 / sizeof(X))));
-    } else {
-        X h[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = i < n ? p[i] : (X)0.0f;
-        r = __builtin_bit_cast(Raw8<X>, h);
-    }
-    return r;
-}
-
 // Zeroes behind the first n.
 template <class X>
 __device__ __forceinline__ void clear_behind(Raw8<X> &r, int n) {
@@ -200,13 +204,6 @@ __device__ __forceinline__ void x_operand_paired(const Raw8<X> &raw, u32x4 (&out
         out[j] = u32x4{__builtin_amdgcn_perm(w[2], w[0], 0x05040100u), __builtin_amdgcn_perm(w[2], w[0], 0x07060302u),
                        __builtin_amdgcn_perm(w[3], w[1], 0x05040100u), __builtin_amdgcn_perm(w[3], w[1], 0x07060302u)};
     }
-}
-
-// v, of which the compiler knows nothing: bytes of a masked word are converted to floats where they stand,
-// not cut out first.
-__device__ __forceinline__ uint32_t as_is(uint32_t v) {
-    asm("" : "+v"(v));
-    return v;
 }
 
 // Whether `rows` rows can be read through one buffer descriptor: on 4 bytes and within 4 GB.

@@ -20,6 +20,7 @@ namespace samd {
 #define SAMD_INLINE __attribute__((always_inline))
 
 constexpr int kGemmStep = 64;
+
 // Index of 16-byte part `c` (0..7) of row `r` in a buffer of rows of 64 16-bit values.  Of 16 rows, 0..7 lie in the lower
 // halves of 256 bytes (all banks), 8..15 in the upper ones, their parts exchanged by r % 8: neither the 16 rows that an
 // operand's lanes read at one c, nor 8 parts of two rows that are 8 apart, meet a bank twice.
@@ -100,15 +101,18 @@ struct TokenTile {
 // 4 neighbouring results of a row, `n` of them in range.
 template <class X>
 __device__ __forceinline__ void store4(X *p, int n, const float (&v)[4]) {
-    if (n >= 4) {
-        Four<X> t;
+    struct {
+        X v[4];
+    } t;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t.v[i] = (X)v[i];
-        *(Four<X> *)p = t;
+    for (int i = 0; i < 4; ++i) t.v[i] = (X)v[i];
+    if (n >= 4) {
+        if constexpr (sizeof(X) == 4) *(u32x4_at4 *)p = __builtin_bit_cast(u32x4, t);
+        else *(u32x2_at2 *)p = __builtin_bit_cast(u32x2, t);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = (X)v[i];
+            if (i < n) p[i] = t.v[i];
     }
 }
 

@@ -39,9 +39,9 @@ __device__ __forceinline__ void pieces_of(float (&v)[8], u32x4 (&out)[P]) {
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         if (j == P - 1) {
-            bf16_t h[8];
+            Eight<bf16_t> h;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = (bf16_t)v[i];
+            for (int i = 0; i < 8; ++i) h.v[i] = (bf16_t)v[i];
             out[j] = __builtin_bit_cast(u32x4, h);
         } else {
 #pragma unroll
@@ -55,11 +55,10 @@ __device__ __forceinline__ void pieces_of(float (&v)[8], u32x4 (&out)[P]) {
 template <class X>
 __device__ __forceinline__ void grad_operand(const Raw8<X> &raw, u32x4 (&out)[kGradPieces<X>]) {
     if constexpr (std::is_same_v<X, half_t>) {
-        half_t h[8];
-        *(u32x4 *)h = raw.v[0];
+        const Eight<half_t> h = __builtin_bit_cast(Eight<half_t>, raw);
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+        for (int i = 0; i < 8; ++i) v[i] = (float)h.v[i];
         pieces_of(v, out);
     } else {
         x_operand(raw, out);

@@ -177,7 +177,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
                 to[0] = __builtin_bit_cast(u32x4, f32x4{v[0], v[2], v[4], v[6]});
                 to[64] = __builtin_bit_cast(u32x4, f32x4{v[1], v[3], v[5], v[7]});
             } else {
-                const X h[8] = {(X)v[0], (X)v[4], (X)v[1], (X)v[5], (X)v[2], (X)v[6], (X)v[3], (X)v[7]};
+                const Eight<X> h = {{(X)v[0], (X)v[4], (X)v[1], (X)v[5], (X)v[2], (X)v[6], (X)v[3], (X)v[7]}};
                 to[0] = __builtin_bit_cast(u32x4, h);
             }
             // four neighbouring threads hold a lane's 32 values
