@@ -73,10 +73,11 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     constexpr int KPT = BN * 8 / THREADS;   // columns of a thread: a half or a quarter of a word
     static_assert(KPT == 2 || KPT == 4, "columns of a thread");
     constexpr int WORDS = BN / 8, GROUPS = BN / 32;   // of a row of the tile; the most groups
+    constexpr int kScaleRow = kGemmStep + 8;          // of one group's column, a quarter of the banks further each
     struct Buffers {
         u32x4 x[2][P][BT * 8], w[2][P][BN * 8];
         u32x4 q[2][kGemmStep * WORDS / 4];        // words as they are stored, 64 rows
-        f32x2 s[2][kGemmStep * GROUPS];           // scales, and scales times zero points
+        f32x2 s[2][GROUPS * kScaleRow];           // scales, and scales times zero points
     };
     static_assert((KS - 1) * BT * BN * 4 <= (int)sizeof(Buffers) * KS, "the slices' sums meet in the buffers");
     __shared__ Buffers all[KS];
@@ -120,10 +121,16 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
         fw.s = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, g * 4, 0, 0));
         if (!SIGNED) fw.z = __builtin_amdgcn_raw_buffer_load_b8(rz, g, 0, 0);
     };
-    // The words' 16-byte parts exchanged by row / 8, the scales by row % 8 and row / 8: the reads below meet few banks twice.
+    // Four words of row 8 c + j: the reads of one j take all c and two neighbouring fours, which fill the 256 bytes of
+    // all banks; the writes take 16 of one c, for which the places are exchanged by the rest.
+    auto four_at = [&](int c, int j, int four) SAMD_INLINE {
+        const int rest = j * (WORDS / 8) + four / 2;
+        return rest * 16 + ((c * 2 + four % 2) ^ (rest % 8 * 2));
+    };
+    auto scale_at = [&](int c, int j, int group) SAMD_INLINE { return group * kScaleRow + j * 8 + c; };
     auto store_words = [&](int buf) SAMD_INLINE {
-        all[slice].q[buf][urow * (WORDS / 4) + (ucol ^ (urow / 8 % (WORDS / 4)))] = fw.q;
-        all[slice].s[buf][(srow % 8 * 8 + srow / 8) * GROUPS + sgroup] = f32x2{fw.s, fw.s * (SIGNED ? 8.0f : (float)fw.z)};
+        all[slice].q[buf][four_at(urow / 8, urow % 8, ucol)] = fw.q;
+        all[slice].s[buf][scale_at(srow / 8, srow % 8, sgroup)] = f32x2{fw.s, fw.s * (SIGNED ? 8.0f : (float)fw.z)};
     };
     // On to the operands, a thread takes KPT columns of 8 rows; eight neighbouring threads different rows.
     const int chunk = tid % 8, column = (tid / 8 % WORDS) * 8 + tid / BN * KPT;
@@ -133,8 +140,8 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
         const uint32_t *q = (const uint32_t *)all[slice].q[buf];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t w = q[(chunk * 8 + j) * WORDS + (word / 4 ^ chunk % (WORDS / 4)) * 4 + word % 4];
-            const f32x2 s = all[slice].s[buf][(j * 8 + chunk) * GROUPS + sgroup_of];
+            const uint32_t w = q[four_at(chunk, j, word / 4) * 4 + word % 4];
+            const f32x2 s = all[slice].s[buf][scale_at(chunk, j, sgroup_of)];
             const uint32_t u = ((w ^ kFlip) >> shift) & (KPT == 4 ? 0xffffu : 0xffu);
             const uint32_t lo = as_is(u & 0x0f0f0f0fu), hi = as_is((u >> 4) & 0x0f0f0f0fu);
 #pragma unroll
