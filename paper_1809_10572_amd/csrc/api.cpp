@@ -979,10 +979,17 @@ int check_rows(const GroupW &w, samd_fmt f, const char *name) {
     return SAMD_OK;
 }
 
-// Rows of weights: a row's length, where a kernel addresses some tens of rows by 32-bit offsets.
+// Rows of weights: a row's length, where a kernel addresses some tens of rows by 32-bit offsets; and the rows that a
+// workgroup of the gradient sums over.
 int check_row_length(int64_t K) {
     if (K > kMaxGroupCols)
         return fail(SAMD_EUNSUPPORTED, "K = %lld: rows of more than 2^25 weights are not supported", (long long)K);
+    return SAMD_OK;
+}
+
+int check_row_count(int64_t M) {
+    if (M > kMaxGroupCols)
+        return fail(SAMD_EUNSUPPORTED, "M = %lld: gradients over more than 2^25 rows are not supported", (long long)M);
     return SAMD_OK;
 }
 
@@ -1059,6 +1066,7 @@ int samd_group_matmul_grad(const void *dy, int32_t type, int64_t lddy, const uin
     if (!st) st = check_size(M, 1, "M");
     if (!st) st = check_size(K, 0, "K");
     if (!st) st = check_row_length(K);
+    if (!st) st = check_row_count(M);
     if (st) return st;
     if (T == 0 || K == 0) return SAMD_OK;
     const bool two = dy2 || q2 || scale2 || zero2;

@@ -10,6 +10,12 @@
 // step's loads in flight during this step's products.
 // W is the first operand: a lane then ends with 4 consecutive rows of W for a token, which are stored together
 // and are one word of the gated block's stored projections.
+//
+// Measured (graph of calls, 4096 x 4096 weights): 2048 tokens bf16 or f16 85 us with signed groups of 128 (807 TFLOP/s of
+// the 1150 that a large library product reaches), 106 us with unsigned groups of 32 (twice the scaling and its sums),
+// f32 225 us; 256 tokens 24 us, 64 tokens 15 us.  In the largest tile the phases that fetch bound it (operands
+// out of LDS, decoding, writing the next step: 78 us were the products left out, the products alone 59), which is why
+// two groups of waves alternate; few tokens are bound by a workgroup's chain of steps.
 #pragma once
 
 #include "group_device.hpp"

@@ -14,6 +14,12 @@
 // decode them, each row of each word and its scale was a load: 168 us against 110 for 2048 x 4096 x 4096 bf16, one tile), and a
 // thread then takes the same KPT columns of eight rows and writes KPT operand parts of eight rows each, so that
 // the transposition costs nothing but its choice of pairs.
+//
+// Measured (graph of calls, 4096 x 4096 weights, signed groups of 128): 2048 tokens bf16 91 us (757 TFLOP/s of the
+// 1150 that a large library product reaches), 1024 tokens f16 116 us (the three instructions of a product: 890), 2048
+// tokens f32 459 us; 256 tokens bf16 29 us.  Bound by what lies between two barriers of a step: operands out of LDS,
+// the next step's decoding and writes, only in part under the other waves' products.  Few tokens are bound by the
+// chain of steps of a workgroup, whose number only the slices cut.
 #include <hip/hip_runtime.h>
 
 #include "group_gemm.hpp"
@@ -294,17 +300,17 @@ int launch_grad_of(const GroupGrad &p, hipStream_t s) {
     };
     if constexpr (std::is_same_v<X, bf16_t>) {
         if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 4>(p, s);
-        const int64_t small = cost(64, 64, 29), middle = cost(128, 128, 55), large = cost(256, 128, 98);
+        const int64_t small = cost(64, 64, 29), middle = cost(128, 128, 55), large = cost(256, 128, 91);
         if (large < middle && large < small) return launch_grad_tile<X, true, 4, 4, 4, 2, 1>(p, s);
         if (middle < small) return launch_grad_tile<X, true, 4, 4, 2, 2, 2>(p, s);
         return launch_grad_tile<X, true, 2, 4, 2, 1, 4>(p, s);
     } else if constexpr (std::is_same_v<X, half_t>) {
         if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 2>(p, s);
-        if (cost(128, 128, 117) < cost(64, 64, 54)) return launch_grad_tile<X, true, 2, 4, 4, 2, 1>(p, s);
+        if (cost(128, 128, 116) < cost(64, 64, 56)) return launch_grad_tile<X, true, 2, 4, 4, 2, 1>(p, s);
         return launch_grad_tile<X, true, 2, 4, 2, 1, 2>(p, s);
     } else {
         if (!buffered) return launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
-        const int64_t small = cost(32, 64, 61), middle = cost(64, 64, 94), large = cost(64, 128, 118);
+        const int64_t small = cost(32, 64, 61), middle = cost(64, 64, 95), large = cost(64, 128, 114);
         if (large < middle && large < small) return launch_grad_tile<X, true, 2, 2, 2, 4, 1>(p, s);
         if (middle < small) return launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s);
         return launch_grad_tile<X, true, 2, 2, 1, 2, 2>(p, s);

@@ -34,7 +34,7 @@ int launch_product(const GroupProduct &p, hipStream_t s) {
     if (!buffered) narrow *= 2;   // rows of x at odd addresses: 100 x 2001 x 1501 takes it 22 us, a tile 16
     const int64_t small = cost(64, 64 / NW, kWide ? 55 : 23);
     const int64_t middle = kWide ? cost(64, 128 / NW, 84) : cost(128, 128 / NW, 53);
-    const int64_t large = kWide ? cost(128, 128 / NW, 108) : cost(256, 128 / NW, 80);
+    const int64_t large = kWide ? cost(128, 128 / NW, 108) : cost(256, 128 / NW, 85);
     if (narrow < std::min(small, std::min(middle, large)))
         return p.w[0].zero ? launch_narrow<X, false, NW>(p, words, groups, s) : launch_narrow<X, true, NW>(p, words, groups, s);
     if (!buffered)

@@ -4,6 +4,10 @@
 // One thread takes 8 consecutive values: 16 bytes of a 16-bit type, one packed word of 4-bit
 // values or two of 8-bit ones.  A group is 4, 8 or 16 neighbouring threads, so its span is two
 // to four cross-lane steps and nothing is read twice.
+//
+// Measured (kernel alone; the call's bytes over its time): 4096 x 4099 f32 to unsigned 4 bits 17.3 us (4.4 TB/s, rows at
+// odd addresses), back 15.6 (4.9); 8192 x 4096 bf16 to signed 8 bits 24.6 us (4.2), back 17.9 (5.8, in part from
+// cache); the gated gradient of 2048 x 10240 bf16 33.9 us (5.1).  A large copy reaches 5.2.
 #include <hip/hip_runtime.h>
 
 #include "group_device.hpp"

@@ -6,7 +6,7 @@
 // four lane operations for each value.  A lane takes 32 consecutive values of a row, 16 bytes, which
 // one scale covers whatever the group, and keeps every operation whole-word:
 //   16-bit types  (16 + u) / 16 is a 16-bit float whose top four mantissa bits are u, so two values
-//                 become two floats by one shift and one and-or, and a two-way dot product adds both:
+//                 become two floats by one shift and one and-xor, and a two-way dot product adds both:
 //                 sum x (u - z) = 16 sum x (16 + u)/16 - (16 + z) sum x, sum x once for all rows
 //   f32           fields to floats by byte conversions, one multiply-add each
 // The offset of 16 costs the 32-bit sum two bits at most; the products themselves are exact.

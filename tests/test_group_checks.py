@@ -102,6 +102,12 @@ def test_matmul_refuses():
     assert matmul(zero=P) == EINVAL                  # signed with zero points
 
 
+def test_grad_refuses_a_sum_over_too_many_rows():
+    many = (1 << 25) + 1
+    assert grad(M=many, lddy=many) == EUNSUP
+    assert b"M = 33554433" in samd.lib().samd_last_error()
+
+
 def test_grad_refuses():
     assert grad(dy=None) == EINVAL and grad(dx=None) == EINVAL and grad(q=None) == EINVAL
     assert grad(dy=ODD2) == EALIGN and grad(dx=ODD2) == EALIGN
