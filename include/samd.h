@@ -559,7 +559,9 @@ int samd_group_matmul(const void *x, int32_t type, int64_t ldx, const uint32_t *
 /* dx = dy W, the gradient of samd_group_matmul with respect to x (W itself is frozen):
  * dy is T x M, dx is T x K.  With dy2 and q2, scale2, zero2 given (all of them, zero2 when
  * wf is unsigned), dx = dy W + dy2 W2, both sums before the one rounding: the input
- * gradient of samd_group_gated.  dy and dy2 have the same row stride. */
+ * gradient of samd_group_gated.  dy and dy2 have the same row stride.  A dy row that holds an
+ * infinity, a NaN or a magnitude that exceeds 2^100 itself or times a scale may give a dx row
+ * of NaN and infinities, as above. */
 int samd_group_matmul_grad(const void *dy, int32_t type, int64_t lddy, const uint32_t *q, const float *scale,
                            const uint8_t *zero, const void *dy2, const uint32_t *q2, const float *scale2,
                            const uint8_t *zero2, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K,

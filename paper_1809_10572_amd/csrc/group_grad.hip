@@ -1,10 +1,14 @@
 // The input gradient of products with 4-bit group-scaled weights on the matrix cores: dx = dy W (+ dy2 W2).
 //
 // The sum runs over the rows of W, and a group's scale differs from row to row, so it is part of the summed product
-// and has to be multiplied into an operand: a weight s (u - z) is computed in 32-bit floats and enters
-//   bf16  as one bf16, rounded: off by at most 2^-8 of each weight, as the types of dy and dx are
-//   f16   as two bf16 of together 16 bits and more, dy as two that hold its 11 bits: three instructions a product
-//   f32   as three bf16 of 8 bits, as is dy: the six largest of their products, off by 2^-24
+// and has to be multiplied into an operand in 32-bit floats, one of two ways:
+//   into the weights   s (u - z) as one bf16, rounded, for bf16 (off by at most 2^-8 of each weight, as the types of dy
+//                      and dx are); f16 as two bf16 of together 16 bits and more, dy as two that hold its 11 bits,
+//                      three instructions a product; f32 as three, as is dy, the six largest of their products
+//   into dy            s dy for each group of the tile's columns, as two bf16 (f16, 16 bits and more) or three (f32, all 24);
+//                      u - z is a whole number, exact as one bf16: two or three instructions, but dy is converted
+//                      once for each group, 64 columns at most.  Groups of 64 and 128, and few tokens in f32: 512 x
+//                      4096 x 4096 f32 113 us to 90; with groups of 32 2048 tokens take 687 us so and 462 the other way
 // (a bf16 holds any float's range; an f16 operand would lose small scales).  Everything is summed in 32-bit floats, both
 // pairs into one sum, and rounded once.
 //
@@ -16,8 +20,8 @@
 // the transposition costs nothing but its choice of pairs.
 //
 // Measured (graph of calls, 4096 x 4096 weights, signed groups of 128): 2048 tokens bf16 91 us (757 TFLOP/s of the
-// 1150 that a large library product reaches), 1024 tokens f16 116 us (the three instructions of a product: 890), 2048
-// tokens f32 459 us; 256 tokens bf16 29 us.  Bound by what lies between two barriers of a step: operands out of LDS,
+// 1150 that a large library product reaches), 1024 tokens f16 108 us, 2048 tokens f32 353 us; 256 tokens bf16 29, f16 49,
+// f32 56 us.  Bound by what lies between two barriers of a step: operands out of LDS,
 // the next step's decoding and writes, only in part under the other waves' products.  Few tokens are bound by the
 // chain of steps of a workgroup, whose number only the slices cut.
 #include <hip/hip_runtime.h>
@@ -28,7 +32,7 @@ namespace samd {
 
 namespace {
 
-// bf16 pieces of dy and of a weight.
+// bf16 pieces of dy, or of dy times a scale.
 template <class X>
 constexpr int kGradPieces = sizeof(X) == 4 ? 3 : std::is_same_v<X, half_t> ? 2 : 1;
 
@@ -58,32 +62,34 @@ __device__ __forceinline__ void pieces_of(float (&v)[8], u32x4 (&out)[P]) {
     }
 }
 
-template <class X>
-__device__ __forceinline__ void grad_operand(const Raw8<X> &raw, u32x4 (&out)[kGradPieces<X>]) {
-    if constexpr (std::is_same_v<X, half_t>) {
-        const Eight<half_t> h = __builtin_bit_cast(Eight<half_t>, raw);
-        float v[8];
+// 8 values of dy, or of dy times their rows' scales, as operands.
+template <class X, int P, class F>
+__device__ __forceinline__ void grad_operand(const Raw8<X> &raw, u32x4 (&out)[P], F &&scale) {
+    const Eight<X> x = __builtin_bit_cast(Eight<X>, raw);
+    float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)h.v[i];
-        pieces_of(v, out);
-    } else {
-        x_operand(raw, out);
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)x.v[i] * scale(i);
+    pieces_of(v, out);
 }
 
-template <class X, bool SIGNED, bool BUF, int WT, int WM, int TW, int MW, int KS>
+// GX: groups of a tile whose scales go into dy; 0: the scales go into the weights.
+template <class X, bool SIGNED, bool BUF, int GX, int WT, int WM, int TW, int MW, int KS>
 __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad p, int words, int groups, int gshift,
                                                                        int tblocks) {
     constexpr int P = kGradPieces<X>, THREADS = 64 * TW * MW;
     constexpr int BT = 16 * WT * TW, BN = 16 * WM * MW;
-    constexpr int KPT = BN * 8 / THREADS;   // columns of a thread: a half or a quarter of a word
+    constexpr int DECODERS = THREADS < BN * 4 ? THREADS : BN * 4;   // threads that decode
+    constexpr int KPT = BN * 8 / DECODERS;   // columns of a thread: a half or a quarter of a word
     static_assert(KPT == 2 || KPT == 4, "columns of a thread");
+    constexpr int DY = GX ? GX : 1;          // operands of dy
+    static_assert(MW % DY == 0, "a wave's columns lie in one group of the tile");
+    constexpr int PW = GX ? 1 : P;           // operands of W
     constexpr int WORDS = BN / 8, GROUPS = BN / 32;   // of a row of the tile; the most groups
     constexpr int kScaleRow = kGemmStep + 8;          // of one group's column, a quarter of the banks further each
     struct Buffers {
-        u32x4 x[2][P][BT * 8], w[2][P][BN * 8];
+        u32x4 x[2][DY][P][BT * 8], w[2][PW][BN * 8];
         u32x4 q[2][kGemmStep * WORDS / 4];        // words as they are stored, 64 rows
-        f32x2 s[2][GROUPS * kScaleRow];           // scales, and scales times zero points
+        f32x2 s[2][GROUPS * kScaleRow];           // scales, and zero points (times scales where those go into the weights)
     };
     static_assert((KS - 1) * BT * BN * 4 <= (int)sizeof(Buffers) * KS, "the slices' sums meet in the buffers");
     __shared__ Buffers all[KS];
@@ -136,12 +142,13 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     auto scale_at = [&](int c, int j, int group) SAMD_INLINE { return group * kScaleRow + j * 8 + c; };
     auto store_words = [&](int buf) SAMD_INLINE {
         all[slice].q[buf][four_at(urow / 8, urow % 8, ucol)] = fw.q;
-        all[slice].s[buf][scale_at(srow / 8, srow % 8, sgroup)] = f32x2{fw.s, fw.s * (SIGNED ? 8.0f : (float)fw.z)};
+        all[slice].s[buf][scale_at(srow / 8, srow % 8, sgroup)] = f32x2{fw.s, (GX ? 1.0f : fw.s) * (SIGNED ? 8.0f : (float)fw.z)};
     };
     // On to the operands, a thread takes KPT columns of 8 rows; eight neighbouring threads different rows.
-    const int chunk = tid % 8, column = (tid / 8 % WORDS) * 8 + tid / BN * KPT;
+    const int chunk = tid % 8, column = (tid / 8 % WORDS) * 8 + tid % DECODERS / BN * KPT;
     const int word = column / 8, shift = column % 8 * 4, sgroup_of = column >> gshift;
     auto decode = [&](int buf) SAMD_INLINE {
+        if (DECODERS < THREADS && tid >= DECODERS) return;
         float v[KPT][8];
         const uint32_t *q = (const uint32_t *)all[slice].q[buf];
 #pragma unroll
@@ -152,16 +159,22 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
             const uint32_t lo = as_is(u & 0x0f0f0f0fu), hi = as_is((u >> 4) & 0x0f0f0f0fu);
 #pragma unroll
             for (int c = 0; c < KPT; c += 2) {
-                v[c][j] = fmaf(s[0], (float)((lo >> (4 * c)) & 255u), -s[1]);
-                v[c + 1][j] = fmaf(s[0], (float)((hi >> (4 * c)) & 255u), -s[1]);
+                const float l = (float)((lo >> (4 * c)) & 255u), h = (float)((hi >> (4 * c)) & 255u);
+                v[c][j] = GX ? l - s[1] : fmaf(s[0], l, -s[1]);
+                v[c + 1][j] = GX ? h - s[1] : fmaf(s[0], h, -s[1]);
             }
         }
 #pragma unroll
         for (int c = 0; c < KPT; ++c) {
-            u32x4 piece[P];
-            pieces_of(v[c], piece);
+            u32x4 piece[PW];
+            if constexpr (GX != 0) {   // whole numbers of at most 4 bits
 #pragma unroll
-            for (int j = 0; j < P; ++j) ws[buf][j][part_at(column + c, chunk)] = piece[j];
+                for (int i = 0; i < 4; ++i) piece[0][i] = upper_halves(v[c][2 * i], v[c][2 * i + 1]);
+            } else {
+                pieces_of(v[c], piece);
+            }
+#pragma unroll
+            for (int j = 0; j < PW; ++j) ws[buf][j][part_at(column + c, chunk)] = piece[j];
         }
     };
     TokenTile<X, BT, THREADS, BUF> fx;
@@ -175,18 +188,33 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     };
     auto store_x = [&](auto ragged, int n, int buf) SAMD_INLINE {
         const int step = step_of(n);
-        fx.template store<decltype(ragged)::value>(xs[buf], p.M, p.dy[1] && step >= single ? step - single : step, tid,
-                                                   [](const Raw8<X> &r, u32x4(&o)[P]) { grad_operand(r, o); });
+        const int at_step = p.dy[1] && step >= single ? step - single : step;
+        if constexpr (GX != 0) {   // a thread's values are those of eight rows of W
+#pragma unroll
+            for (int g = 0; g < DY; ++g) {
+                float scale[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) scale[j] = all[slice].s[buf][scale_at(chunk, j, g)][0];
+                fx.template store<decltype(ragged)::value>(xs[buf][g], p.M, at_step, tid, [&](const Raw8<X> &r, u32x4(&o)[P]) SAMD_INLINE {
+                    grad_operand(r, o, [&](int j) SAMD_INLINE { return scale[j]; });
+                });
+            }
+        } else {
+            fx.template store<decltype(ragged)::value>(xs[buf][0], p.M, at_step, tid, [](const Raw8<X> &r, u32x4(&o)[P]) {
+                if constexpr (std::is_same_v<X, half_t>) grad_operand(r, o, [](int) { return 1.0f; });
+                else x_operand(r, o);
+            });
+        }
     };
 
     const int at[2] = {part_at(low, quarter), part_at(low, 4 + quarter)};   // the same in every 16 rows
     f32x4 acc[WM][WT] = {};
-    u32x4 av[2][P][WM];
+    u32x4 av[2][PW][WM];
     auto operands = [&](int buf) SAMD_INLINE {
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int j = 0; j < P; ++j)
+            for (int j = 0; j < PW; ++j)
 #pragma unroll
                 for (int i = 0; i < WM; ++i) av[c][j][i] = ws[buf][j][(mw * WM + i) * 128 + at[c]];
     };
@@ -199,7 +227,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
                 for (int j = 0; j < P; ++j) {
                     const u32x4 bv = x_of(c, j, t);
 #pragma unroll
-                    for (int h = 0; h < P - j; ++h)   // pieces j and h: 2^-8(j + h) of the product
+                    for (int h = 0; h < (GX ? 1 : P - j); ++h)   // pieces j and h: 2^-8(j + h) of the product
 #pragma unroll
                         for (int i = 0; i < WM; ++i) acc[i][t] = mfma<bf16_t>(av[c][h][i], bv, acc[i][t]);
                 }
@@ -212,12 +240,12 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     load_x(0);
     store_words(0);
     load_words(1);
+    __syncthreads();
     store_x(std::true_type{}, 0, 0);
     load_x(1);
+    decode(0);
     store_words(1);
     load_words(2);
-    __syncthreads();
-    decode(0);
     __syncthreads();
     auto ahead = [&](auto ragged, int n, int buf) SAMD_INLINE {   // while position n, in buffer buf, is multiplied
         store_x(ragged, n + 1, buf ^ 1);
@@ -227,7 +255,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
         load_words(n + 3);
     };
     auto both = [&](auto ragged, int n, int buf) SAMD_INLINE {
-        auto x_of = [&](int c, int j, int t) SAMD_INLINE { return xs[buf][j][(tw * WT + t) * 128 + at[c]]; };
+        auto x_of = [&](int c, int j, int t) SAMD_INLINE { return xs[buf][mw * DY / MW][j][(tw * WT + t) * 128 + at[c]]; };
         operands(buf);
         multiply(x_of, 0, WT / 2);
         ahead(ragged, n, buf);
@@ -270,7 +298,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     }
 }
 
-template <class X, bool BUF, int WT, int WM, int TW, int MW, int KS>
+template <class X, bool BUF, int GX, int WT, int WM, int TW, int MW, int KS>
 int launch_grad_tile(const GroupGrad &p, hipStream_t s) {
     constexpr int BT = 16 * WT * TW, BN = 16 * WM * MW;
     const int words = (int)row_words(p.K, 4), groups = (p.K + p.group - 1) / p.group;
@@ -283,7 +311,8 @@ int launch_grad_tile(const GroupGrad &p, hipStream_t s) {
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * TW * MW * KS), 0, s, p, words, groups, gshift, (int)tblocks);
     };
-    p.w[0].zero ? go(group_grad_kernel<X, false, BUF, WT, WM, TW, MW, KS>) : go(group_grad_kernel<X, true, BUF, WT, WM, TW, MW, KS>);
+    p.w[0].zero ? go(group_grad_kernel<X, false, BUF, GX, WT, WM, TW, MW, KS>)
+                : go(group_grad_kernel<X, true, BUF, GX, WT, WM, TW, MW, KS>);
     return check_launch("samd_group_matmul_grad");
 }
 
@@ -299,21 +328,33 @@ int launch_grad_of(const GroupGrad &p, hipStream_t s) {
         return (blocks + 255) / 256 * unit;
     };
     if constexpr (std::is_same_v<X, bf16_t>) {
-        if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 4>(p, s);
+        if (!buffered) return launch_grad_tile<X, false, 0, 2, 4, 2, 1, 4>(p, s);
         const int64_t small = cost(64, 64, 29), middle = cost(128, 128, 55), large = cost(256, 128, 91);
-        if (large < middle && large < small) return launch_grad_tile<X, true, 4, 4, 4, 2, 1>(p, s);
-        if (middle < small) return launch_grad_tile<X, true, 4, 4, 2, 2, 2>(p, s);
-        return launch_grad_tile<X, true, 2, 4, 2, 1, 4>(p, s);
+        if (large < middle && large < small) return launch_grad_tile<X, true, 0, 4, 4, 4, 2, 1>(p, s);
+        if (middle < small) return launch_grad_tile<X, true, 0, 4, 4, 2, 2, 2>(p, s);
+        return launch_grad_tile<X, true, 0, 2, 4, 2, 1, 4>(p, s);
     } else if constexpr (std::is_same_v<X, half_t>) {
-        if (!buffered) return launch_grad_tile<X, false, 2, 4, 2, 1, 2>(p, s);
-        if (cost(128, 128, 116) < cost(64, 64, 56)) return launch_grad_tile<X, true, 2, 4, 4, 2, 1>(p, s);
-        return launch_grad_tile<X, true, 2, 4, 2, 1, 2>(p, s);
+        if (p.group == 32) {
+            if (!buffered) return launch_grad_tile<X, false, 0, 2, 2, 2, 2, 2>(p, s);
+            if (cost(128, 128, 116) < cost(64, 64, 54)) return launch_grad_tile<X, true, 0, 2, 4, 4, 2, 1>(p, s);
+            return launch_grad_tile<X, true, 0, 2, 2, 2, 2, 2>(p, s);
+        }
+        if (!buffered) return launch_grad_tile<X, false, 1, 2, 2, 2, 2, 2>(p, s);
+        if (cost(256, 64, 108) < cost(64, 64, 49)) return launch_grad_tile<X, true, 1, 4, 2, 4, 2, 1>(p, s);
+        return launch_grad_tile<X, true, 1, 2, 2, 2, 2, 2>(p, s);
     } else {
-        if (!buffered) return launch_grad_tile<X, false, 2, 2, 2, 2, 1>(p, s);
-        const int64_t small = cost(32, 64, 61), middle = cost(64, 64, 95), large = cost(64, 128, 114);
-        if (large < middle && large < small) return launch_grad_tile<X, true, 2, 2, 2, 4, 1>(p, s);
-        if (middle < small) return launch_grad_tile<X, true, 2, 2, 2, 2, 1>(p, s);
-        return launch_grad_tile<X, true, 2, 2, 1, 2, 2>(p, s);
+        if (p.group == 32) {
+            const int64_t small = cost(32, 64, 52), middle = cost(64, 64, 85), large = cost(64, 128, 114);
+            if (!buffered) return launch_grad_tile<X, false, 2, 1, 2, 2, 2, 2>(p, s);
+            if (large < middle && large < small) return launch_grad_tile<X, true, 0, 2, 2, 2, 4, 1>(p, s);
+            if (middle < small) return launch_grad_tile<X, true, 2, 1, 2, 4, 2, 1>(p, s);
+            return launch_grad_tile<X, true, 2, 1, 2, 2, 2, 2>(p, s);
+        }
+        const int64_t small = cost(32, 64, 42), middle = cost(64, 64, 56), large = cost(128, 64, 89);
+        if (!buffered) return launch_grad_tile<X, false, 1, 1, 2, 2, 2, 2>(p, s);
+        if (large < middle && large < small) return launch_grad_tile<X, true, 1, 2, 2, 4, 2, 1>(p, s);
+        if (middle < small) return launch_grad_tile<X, true, 1, 2, 2, 2, 2, 2>(p, s);
+        return launch_grad_tile<X, true, 1, 1, 2, 2, 2, 2>(p, s);
     }
 }
 
