@@ -20,10 +20,10 @@
 // the transposition costs nothing but its choice of pairs.
 //
 // Measured (graph of calls, 4096 x 4096 weights, signed groups of 128): 2048 tokens bf16 91 us (757 TFLOP/s of the
-// 1150 that a large library product reaches), 1024 tokens f16 108 us, 2048 tokens f32 353 us; 256 tokens bf16 29, f16 49,
-// f32 56 us.  Bound by what lies between two barriers of a step: operands out of LDS,
-// the next step's decoding and writes, only in part under the other waves' products.  Few tokens are bound by the
-// chain of steps of a workgroup, whose number only the slices cut.
+// 1150 that a large library product reaches), f32 353 us, 1024 tokens f16 108 us; 128 tokens bf16 29 us, f16 35, f32 39.
+// Bound by what lies between two barriers of a step (operands out of LDS, the next step's decoding and writes), only in
+// part under the other waves' products.  Few tokens are bound by the chain of steps of a workgroup, whose number only
+// the slices cut: as many as LDS holds.
 #include <hip/hip_runtime.h>
 
 #include "group_gemm.hpp"
@@ -340,8 +340,10 @@ int launch_grad_of(const GroupGrad &p, hipStream_t s) {
             return launch_grad_tile<X, true, 0, 2, 2, 2, 2, 2>(p, s);
         }
         if (!buffered) return launch_grad_tile<X, false, 1, 2, 2, 2, 2, 2>(p, s);
-        if (cost(256, 64, 108) < cost(64, 64, 49)) return launch_grad_tile<X, true, 1, 4, 2, 4, 2, 1>(p, s);
-        return launch_grad_tile<X, true, 1, 2, 2, 2, 2, 2>(p, s);
+        const int64_t small = cost(32, 64, 37), middle = cost(64, 64, 49), large = cost(256, 64, 108);
+        if (large < middle && large < small) return launch_grad_tile<X, true, 1, 4, 2, 4, 2, 1>(p, s);
+        if (middle < small) return launch_grad_tile<X, true, 1, 2, 2, 2, 2, 2>(p, s);
+        return launch_grad_tile<X, true, 1, 1, 2, 2, 2, 4>(p, s);
     } else {
         if (p.group == 32) {
             const int64_t small = cost(32, 64, 52), middle = cost(64, 64, 85), large = cost(64, 128, 114);
@@ -350,11 +352,11 @@ int launch_grad_of(const GroupGrad &p, hipStream_t s) {
             if (middle < small) return launch_grad_tile<X, true, 2, 1, 2, 4, 2, 1>(p, s);
             return launch_grad_tile<X, true, 2, 1, 2, 2, 2, 2>(p, s);
         }
-        const int64_t small = cost(32, 64, 42), middle = cost(64, 64, 56), large = cost(128, 64, 89);
+        const int64_t small = cost(32, 64, 40), middle = cost(64, 64, 56), large = cost(128, 64, 89);
         if (!buffered) return launch_grad_tile<X, false, 1, 1, 2, 2, 2, 2>(p, s);
         if (large < middle && large < small) return launch_grad_tile<X, true, 1, 2, 2, 4, 2, 1>(p, s);
         if (middle < small) return launch_grad_tile<X, true, 1, 2, 2, 2, 2, 2>(p, s);
-        return launch_grad_tile<X, true, 1, 1, 2, 2, 2, 2>(p, s);
+        return launch_grad_tile<X, true, 1, 1, 2, 2, 2, 3>(p, s);
     }
 }
 
