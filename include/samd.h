@@ -526,7 +526,9 @@ int samd_scale(const uint32_t *a, int64_t nwords, samd_fmt f, int32_t scalar, ui
  * start on 16 bytes are read and written fastest.  Sums and scales are 32-bit floats
  * whatever the type; a result is rounded once, to the type, unless a call says more.
  * Sizes are at most 2^31 - 1 each (K, a row of weights, and M of samd_group_matmul_grad at
- * most 2^25: SAMD_EUNSUPPORTED), offsets are 64-bit.  Inputs and outputs must not overlap.
+ * most 2^25, and a result of so many values that its launch would need 2^32 threads, some
+ * 10^8 rows of weights for a token: SAMD_EUNSUPPORTED), offsets are 64-bit.  Inputs and
+ * outputs must not overlap.
  * No call needs a workspace, and a call's results do not depend on what else runs: no
  * atomics, a fixed order of every sum. */
 enum { SAMD_F32 = 0, SAMD_F16 = 1, SAMD_BF16 = 2 };

@@ -206,6 +206,15 @@ __device__ __forceinline__ void x_operand_paired(const Raw8<X> &raw, u32x4 (&out
     }
 }
 
+// Whether a launch of `blocks` workgroups is possible: below 2^32 threads.
+inline int check_blocks(int64_t blocks, int threads, const char *call) {
+    if (blocks > UINT32_MAX / threads) {
+        set_error(std::string(call) + ": a result of so many values needs 2^32 threads or more in one launch");
+        return SAMD_EUNSUPPORTED;
+    }
+    return SAMD_OK;
+}
+
 // Whether `rows` rows can be read through one buffer descriptor: on 4 bytes and within 4 GB.
 inline bool within_buffer(const void *p, int64_t size, int64_t rows, int64_t ld, int64_t cols) {
     return ((uintptr_t)p & 3) == 0 && ld * size % 4 == 0 && ((__int128)rows * ld + cols) * size < (__int128)0xff000000;

@@ -379,10 +379,7 @@ template <class X, bool BUF, int NW, int WT, int WM, int TW, int MW, int KS>
 int launch_gemm_tile(const GroupProduct &p, int words, int groups, hipStream_t s) {
     constexpr int BT = 16 * WT * TW, OM = 16 * WM * MW / NW;
     const int64_t tblocks = ((int64_t)p.T + BT - 1) / BT, blocks = tblocks * (((int64_t)p.M + OM - 1) / OM);
-    if (blocks > INT32_MAX) {
-        set_error("group product: T x M needs too many workgroups");
-        return SAMD_EUNSUPPORTED;
-    }
+    if (const int st = check_blocks(blocks, 64 * TW * MW * KS, "group product")) return st;
     auto go = [&](auto per) {
         hipLaunchKernelGGL((group_gemm_kernel<X, BUF, decltype(per)::value, NW, WT, WM, TW, MW, KS>), dim3((uint32_t)blocks),
                            dim3(64 * TW * MW * KS), 0, s, p, words, groups, (int)tblocks);

@@ -304,10 +304,7 @@ int launch_grad_tile(const GroupGrad &p, hipStream_t s) {
     const int words = (int)row_words(p.K, 4), groups = (p.K + p.group - 1) / p.group;
     const int gshift = p.group == 32 ? 5 : p.group == 64 ? 6 : 7;
     const int64_t tblocks = ((int64_t)p.T + BT - 1) / BT, blocks = tblocks * (((int64_t)p.K + BN - 1) / BN);
-    if (blocks > INT32_MAX) {
-        set_error("samd_group_matmul_grad: T x K needs too many workgroups");
-        return SAMD_EUNSUPPORTED;
-    }
+    if (const int st = check_blocks(blocks, 64 * TW * MW * KS, "samd_group_matmul_grad")) return st;
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * TW * MW * KS), 0, s, p, words, groups, gshift, (int)tblocks);
     };

@@ -249,10 +249,7 @@ int launch_narrow(const GroupProduct &p, int words, int groups, hipStream_t s) {
     const int64_t tblocks = ((int64_t)p.T + 16 * tt - 1) / (16 * tt);
     const int mt = NW == 1 && tblocks * (((int64_t)p.M + 15) / 16) >= 512 ? 2 : 1;
     const int64_t blocks = tblocks * (((int64_t)p.M + 16 * mt - 1) / (16 * mt));
-    if (blocks > INT32_MAX) {
-        set_error("group product: T x M needs too many workgroups");
-        return SAMD_EUNSUPPORTED;
-    }
+    if (const int st = check_blocks(blocks, 64 * kNarrowWaves, "group product")) return st;
     const bool buffered = within_buffer(p.x, sizeof(X), std::min<int64_t>(p.T, 32), p.ldx, p.K);
     // a step's zero points (4 bytes for groups of 32, 2 for groups of 64) in one access
     bool whole_zeros = groups % (128 / p.group) == 0;

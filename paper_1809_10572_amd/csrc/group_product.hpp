@@ -14,9 +14,8 @@ int launch_product(const GroupProduct &p, hipStream_t s) {
     // One or two tokens: a row of W a wave (two tokens 4096 x 4096: 5.5 us, on the matrix cores 5.9; with three or four
     // tokens those are ahead: 8192 x 8192 unsigned groups of 64 21.1 and 17.7 us).
     if (p.T <= 2 && !p.g8) {
-        p.w[0].zero ? launch_vector<X, false, NW>(p, words, groups, gshift, s)
-                    : launch_vector<X, true, NW>(p, words, groups, gshift, s);
-        return check_launch("group product");
+        return p.w[0].zero ? launch_vector<X, false, NW>(p, words, groups, gshift, s)
+                           : launch_vector<X, true, NW>(p, words, groups, gshift, s);
     }
     // Up to 16: one operand of tokens, W from memory into operands.
     if (p.T <= 16 && !p.g8)

@@ -214,11 +214,13 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
 // often, unless that leaves CUs without a workgroup (1024 x 16384 weights: 7.4 us with one row a wave,
 // 9.5 with two; 16384 x 8192: 17.7 and 14.8).
 template <class X, bool SIGNED, int NW>
-void launch_vector(const GroupProduct &p, int words, int groups, int gshift, hipStream_t s) {
+int launch_vector(const GroupProduct &p, int words, int groups, int gshift, hipStream_t s) {
     const int steps = (words + 255) / 256;
     const bool one = p.M <= 2048;
     const int rows = kVecWaves * (one ? 1 : 2);
-    const dim3 grid((uint32_t)(((int64_t)p.M + rows - 1) / rows));
+    const int64_t blocks = ((int64_t)p.M + rows - 1) / rows;
+    if (const int st = check_blocks(blocks, 64 * kVecWaves, "group product")) return st;
+    const dim3 grid((uint32_t)blocks);
     auto go = [&](auto kernel, int tokens) {
         const int step_bytes = tokens * (kVecStep * (int)sizeof(X) + 256);
         const int held = std::min(steps, std::max(2, kVecLds / step_bytes & ~1));
@@ -226,6 +228,7 @@ void launch_vector(const GroupProduct &p, int words, int groups, int gshift, hip
     };
     if (p.T == 1) one ? go(group_vector_kernel<X, SIGNED, 1, NW, 1>, 1) : go(group_vector_kernel<X, SIGNED, 1, NW, 2>, 1);
     else one ? go(group_vector_kernel<X, SIGNED, 2, NW, 1>, 2) : go(group_vector_kernel<X, SIGNED, 2, NW, 2>, 2);
+    return check_launch("group product");
 }
 
 }  // namespace samd

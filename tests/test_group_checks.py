@@ -119,6 +119,18 @@ def test_grad_refuses():
     assert grad(dy2=ODD2, q2=P, scale2=P) == EALIGN and grad(dy2=P, q2=ODD1, scale2=P) == EALIGN
 
 
+@pytest.mark.parametrize("type", [F32, F16])
+@pytest.mark.parametrize("T", [1, 2, 16, 40, (1 << 31) - 1])
+def test_results_of_too_many_workgroups_are_refused(type, T):
+    """Launches of 2^32 threads and more are refused before they are made."""
+    big = (1 << 31) - 1 if T <= 40 else 1 << 20
+    assert matmul(type=type, T=T, M=big, ldy=big) == EUNSUP
+    assert gated(type=type, T=T, M=big, ldh=big) == EUNSUP
+    assert b"2^32 threads" in samd.lib().samd_last_error()
+    if T > 40:
+        assert grad(type=type, T=T, K=big, lddx=big) == EUNSUP
+
+
 def test_gated_refuses():
     assert gated(act=2) == EINVAL and gated(act=-1) == EINVAL
     assert gated(qu=None) == EINVAL and gated(su=None) == EINVAL and gated(zu=P) == EINVAL and gated(qg=ODD1) == EALIGN
