@@ -93,11 +93,17 @@ __device__ __forceinline__ void store8(X *p, int n, const float (&v)[8]) {
     }
 }
 
-// A buffer descriptor of `bytes` bytes, filled up to a whole word (a word that holds the last value is
-// read whole, from within one page): reads of words behind them give 0.
+// A buffer descriptor of `bytes` bytes from p on, which is on 4 bytes, filled up to a whole word (a word that holds the
+// last value is read whole, from within one page): reads of words behind them give 0.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, int64_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(uint32_t)min((bytes + 3) & ~(int64_t)3, (int64_t)0xfffffffc),
                                              0x00020000);
+}
+
+// The same for zero points, which are read by bytes and may start anywhere: exactly those bytes, since the words that
+// they are filled up to from such a start could reach into another page.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t byte_buffer_of(const uint8_t *p, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(uint32_t)min(bytes, (int64_t)0xfffffffc), 0x00020000);
 }
 
 // Which row an item of a row-major range belongs to: a multiplication where all items are

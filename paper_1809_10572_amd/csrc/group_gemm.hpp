@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_gemm_kernel(GroupProd
     const bool has_zero = p.w[0].zero != nullptr;
     const uint32_t flip = has_zero ? 0u : 0x88888888u;
     const __amdgpu_buffer_rsrc_t rq = buffer_of(p.w[a].q + m0 * words, (int64_t)rows * words * 4);
-    const __amdgpu_buffer_rsrc_t rz = buffer_of(p.w[a].zero + m0 * groups, has_zero ? (int64_t)rows * groups : 0);
+    const __amdgpu_buffer_rsrc_t rz = byte_buffer_of(p.w[a].zero + m0 * groups, has_zero ? (int64_t)rows * groups : 0);
     const uint32_t qrow = (uint32_t)row * (uint32_t)words, zrow = (uint32_t)row * (uint32_t)groups;
     // scales: a thread loads those of row tid % BM of the buffer
     static_assert(THREADS % BM == 0, "a thread loads the scales of one row");

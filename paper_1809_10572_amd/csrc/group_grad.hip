@@ -127,7 +127,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
         const GroupW &w = p.w[second ? 1 : 0];
         const __amdgpu_buffer_rsrc_t rq = buffer_of(w.q + m0 * words, rows * words * 4);
         const __amdgpu_buffer_rsrc_t rs = buffer_of(w.scale + m0 * groups, rows * groups * 4);
-        const __amdgpu_buffer_rsrc_t rz = buffer_of(w.zero + m0 * groups, SIGNED ? 0 : rows * groups);
+        const __amdgpu_buffer_rsrc_t rz = byte_buffer_of(w.zero + m0 * groups, SIGNED ? 0 : rows * groups);
         fw.q = __builtin_amdgcn_raw_buffer_load_b128(rq, ((uint32_t)urow * (uint32_t)words + (uint32_t)(k0 / 8) + ucol * 4) * 4, 0, 0);
         const uint32_t g = (uint32_t)srow * (uint32_t)groups + (uint32_t)min(g0 + sgroup, groups - 1);
         fw.s = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, g * 4, 0, 0));

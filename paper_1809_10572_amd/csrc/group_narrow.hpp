@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
     for (int a = 0; a < NW; ++a) {
         rq[a] = buffer_of(p.w[a].q + m0 * words, (int64_t)rows * words * 4);
         rs[a] = buffer_of(p.w[a].scale + m0 * groups, (int64_t)rows * groups * 4);
-        rz[a] = buffer_of(p.w[a].zero + m0 * groups, SIGNED ? 0 : (int64_t)rows * groups);
+        rz[a] = byte_buffer_of(p.w[a].zero + m0 * groups, SIGNED ? 0 : (int64_t)rows * groups);
     }
     uint32_t qrow[MT], srow[MT];
 #pragma unroll

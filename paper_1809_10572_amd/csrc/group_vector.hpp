@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
     for (int a = 0; a < NW; ++a) {
         rq[a] = buffer_of(p.w[a].q + first * words, (int64_t)rows * words * 4);
         rs[a] = buffer_of(p.w[a].scale + first * groups, (int64_t)rows * groups * 4);
-        rz[a] = buffer_of(p.w[a].zero + first * groups, SIGNED ? 0 : (int64_t)rows * groups);
+        rz[a] = byte_buffer_of(p.w[a].zero + first * groups, SIGNED ? 0 : (int64_t)rows * groups);
     }
     struct Step {
         u32x4 w[NW][R];
