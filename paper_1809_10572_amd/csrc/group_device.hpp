@@ -139,6 +139,31 @@ __device__ __forceinline__ GroupStep group_step(float span, uint32_t bits, float
     return s;
 }
 
+// The 8 fields of a word less their zero point as 16-bit floats, exactly: pairs of fields i and i + 4, i = 0 .. 3.  A field
+// put under the bits of 1024 is 1024 + u (one that stands four bits higher, 1024 + 16 u); the rest is a subtraction of
+// whole numbers, or a multiply-add with 1/16.  Signed fields have their sign bit flipped: u is the value plus 8.
+struct ZeroPoint {
+    half2_t less, less16;   // -(1024 + z), -(64 + z)
+};
+template <bool SIGNED>
+__device__ __forceinline__ ZeroPoint zero_point(uint32_t z) {   // of 0 .. 255
+    if (SIGNED) z = 8;
+    const half2_t at1024 = __builtin_bit_cast(half2_t, z * 0x00010001u + 0x64006400u);
+    const half2_t k960 = {(half_t)960.0f, (half_t)960.0f};
+    return {-at1024, k960 - at1024};
+}
+template <bool SIGNED>
+__device__ __forceinline__ void whole_pairs(uint32_t w, const ZeroPoint &z, half2_t (&out)[4]) {
+    // as unknown values, so that `and` and `xor` with them are one operation
+    const uint32_t one = as_is(SIGNED ? 0x64086408u : 0x64006400u), sixteen = SIGNED ? as_is(0x64806480u) : one;
+    const half2_t sixteenth = {(half_t)0.0625f, (half_t)0.0625f};
+    const uint32_t v = w >> 8;
+    out[0] = __builtin_bit_cast(half2_t, (w & 0x000f000fu) ^ one) + z.less;
+    out[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (w & 0x00f000f0u) ^ sixteen), sixteenth, z.less16);
+    out[2] = __builtin_bit_cast(half2_t, (v & 0x000f000fu) ^ one) + z.less;
+    out[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (v & 0x00f000f0u) ^ sixteen), sixteenth, z.less16);
+}
+
 // The gated block's activation: a = act(g), da = act'(g).  With the 32-bit exponential and
 // error function, whose errors of a few units in the last place are far below the type's.
 __device__ __forceinline__ void activation(int act, float g, float &a, float &da) {

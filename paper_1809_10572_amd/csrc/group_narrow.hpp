@@ -37,6 +37,16 @@ __device__ __forceinline__ void swap_rows(u32x4 &w) {
     w[A] = r[0], w[B] = r[1];
 }
 
+// Fields i and i + 4 of a word as the floats (16 + u) / 16 of the type; `one` is two floats 1, with their top
+// mantissa bit set where the fields are signed (which flips the field's sign bit: u is the value plus 8).
+template <class X, int I>
+__device__ __forceinline__ uint32_t field_pair(uint32_t w, uint32_t one) {
+    constexpr int kAt = std::is_same_v<X, half_t> ? 6 : 3;   // lowest of the top four mantissa bits
+    constexpr int kShift = kAt - 4 * I;
+    const uint32_t t = kShift >= 0 ? w << (kShift >= 0 ? kShift : 0) : w >> (kShift < 0 ? -kShift : 0);
+    return (t & (0x000f000fu << kAt)) ^ one;
+}
+
 template <class X, bool SIGNED, int PER, int TT, int NW, int MT>
 __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupProduct p, int words, int groups,
                                                                          bool buffered, bool whole_zeros) {

@@ -65,3 +65,54 @@ def test_zero_points_at_any_byte(T, group):
             assert torch.equal(samd.group_matmul(x, vg), y), (typ, off)
             assert torch.equal(samd.group_gated(x, vg, vu), h), (typ, off)
             assert torch.equal(samd.group_matmul_grad(dy, vg, dy, vu), dx), (typ, off)
+
+
+# ---- weights equal to their zero points -----------------------------------------------------------
+
+def rounding(typ, want):
+    """The rounding of 64-bit results to a type: half a step of their value, and, below the type's smallest normal number
+    m, where steps no longer shrink, half of m eps: for f16 2^-14 2^-10 / 2 = 2^-25."""
+    t = torch.finfo(TYPES[typ])
+    return torch.clamp(want.abs(), min=t.smallest_normal) * (t.eps / 2)
+
+
+def near_zero_points(gen, rows, cols, group, zero, ones):
+    """Rows whose fields all equal their zero point, but for `ones` of each row, which lie one step above (below, where the
+    zero point is 15)."""
+    groups = -(-cols // group)
+    if zero == "any":
+        z = torch.randint(0, 16, (rows, groups), generator=gen, device=DEV)
+    else:
+        z = torch.full((rows, groups), 8 if zero is None else zero, device=DEV)
+    q = z.repeat_interleave(group, 1)[:, :cols].clone()
+    if ones:
+        at = torch.randint(0, cols, (rows, ones), generator=gen, device=DEV)
+        q.scatter_(1, at, q.gather(1, at) + torch.where(q.gather(1, at) == 15, -1, 1))
+    if zero is None:
+        q = q ^ 8   # two's complement of the field less 8
+    return from_fields(gen, q, group, None if zero is None else z.to(torch.uint8))
+
+
+def product_is_the_formulas(typ, T, K, M=70):
+    """Nothing from weights that are nothing, and a bound that counts the others alone: at most K/32 + 64 additions and
+    roundings of 2^-24 each of the sum of their magnitudes, and the result's rounding."""
+    gen = torch.Generator(device=DEV).manual_seed(T + K)
+    # of one sign, over twelve powers of two: sums whose bits do not all fit, whatever the type
+    x = torch.exp2(12 * torch.rand(T, K, generator=gen, device=DEV) - 10).to(TYPES[typ])
+    for group in (32, 64, 128):
+        for zero in (None, 0, 3, 15, "any"):
+            w, _ = near_zero_points(gen, M, K, group, zero, 0)
+            assert not samd.group_matmul(x, w).any(), (group, zero)
+            assert not samd.group_gated(x, w, w).any(), (group, zero)
+            w, values = near_zero_points(gen, M, K, group, zero, 3)
+            want = x.double() @ values.t()
+            bound = rounding(typ, want) + (K / 32 + 64) * 2.0 ** -24 * (x.double() @ values.abs().t())
+            off = ((samd.group_matmul(x, w).double() - want).abs() - bound).max().item()
+            assert off <= 0, (group, zero, off)
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("K", [256, 2051, 4100])
+@pytest.mark.parametrize("T", [1, 2])
+def test_products_of_one_and_two_tokens(typ, T, K):
+    product_is_the_formulas(typ, T, K)
