@@ -152,16 +152,50 @@ __device__ __forceinline__ ZeroPoint zero_point(uint32_t z) {   // of 0 .. 255
     const half2_t k960 = {(half_t)960.0f, (half_t)960.0f};
     return {-at1024, k960 - at1024};
 }
+// The fields as such, put under bits: 1024 + u in [0] and [2], 1024 + 16 u in [1] and [3].
 template <bool SIGNED>
-__device__ __forceinline__ void whole_pairs(uint32_t w, const ZeroPoint &z, half2_t (&out)[4]) {
+__device__ __forceinline__ void field_pairs(uint32_t w, half2_t (&out)[4]) {
     // as unknown values, so that `and` and `xor` with them are one operation
     const uint32_t one = as_is(SIGNED ? 0x64086408u : 0x64006400u), sixteen = SIGNED ? as_is(0x64806480u) : one;
-    const half2_t sixteenth = {(half_t)0.0625f, (half_t)0.0625f};
     const uint32_t v = w >> 8;
-    out[0] = __builtin_bit_cast(half2_t, (w & 0x000f000fu) ^ one) + z.less;
-    out[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (w & 0x00f000f0u) ^ sixteen), sixteenth, z.less16);
-    out[2] = __builtin_bit_cast(half2_t, (v & 0x000f000fu) ^ one) + z.less;
-    out[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (v & 0x00f000f0u) ^ sixteen), sixteenth, z.less16);
+    out[0] = __builtin_bit_cast(half2_t, (w & 0x000f000fu) ^ one);
+    out[1] = __builtin_bit_cast(half2_t, (w & 0x00f000f0u) ^ sixteen);
+    out[2] = __builtin_bit_cast(half2_t, (v & 0x000f000fu) ^ one);
+    out[3] = __builtin_bit_cast(half2_t, (v & 0x00f000f0u) ^ sixteen);
+}
+template <bool SIGNED>
+__device__ __forceinline__ void whole_pairs(uint32_t w, const ZeroPoint &z, half2_t (&out)[4]) {
+    const half2_t sixteenth = {(half_t)0.0625f, (half_t)0.0625f};
+    field_pairs<SIGNED>(w, out);
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        out[i] += z.less;
+        out[i + 1] = __builtin_elementwise_fma(out[i + 1], sixteenth, z.less16);
+    }
+}
+
+// The same as a matrix operand of f16 or bf16, whose 8 bits hold every difference of 4 bits and a byte too: each difference
+// by one multiply-add from f16 to f32, the upper halves of two.
+template <class H, bool SIGNED>
+__device__ __forceinline__ u32x4 whole_operand(uint32_t w, const ZeroPoint &z) {
+    half2_t v[4];
+    u32x4 out;
+    if constexpr (std::is_same_v<H, half_t>) {
+        whole_pairs<SIGNED>(w, z, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(uint32_t, v[i]);
+    } else {
+        field_pairs<SIGNED>(w, v);
+        const float one = as_float(1.0f);   // an unknown value: the multiply-add reads f16, an addition would not
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const half2_t less = i % 2 ? z.less16 : z.less;
+            const float k = i % 2 ? 0.0625f : one;
+            const float lo = fmaf((float)v[i][0], k, (float)less[0]), hi = fmaf((float)v[i][1], k, (float)less[1]);
+            out[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+        }
+    }
+    return out;
 }
 
 // The gated block's activation: a = act(g), da = act'(g).  With the 32-bit exponential and

@@ -5,9 +5,8 @@
 // instruction sums over.  A step is 128 values of a row, 16 words, four neighbouring ones to a lane; which of them an
 // instruction takes is free as long as both operands agree and all lie in one group, so groups of 128 need no
 // exchange, groups of 64 and 32 one or two exchanges between halves and rows of lanes (PER = group / 32 instructions
-// a group).  As in the products of few tokens a field becomes the 16-bit float (16 + u) / 16
-// by half an operation, and an instruction on an operand of ones gives each token's sum of x:
-//   y += 16 s (sum x (16 + u)/16 - (1 + z/16) sum x)     once a group, in 32-bit floats.
+// a group).  A field becomes the 16-bit float u - z exactly, by one to two operations; a group's sum is scaled once, in
+// 32-bit floats.
 // 32-bit activations enter as three bf16 pieces of 8 bits each, which hold all 24 bits: the products stay
 // exact, three instructions for each.
 //
@@ -37,16 +36,6 @@ __device__ __forceinline__ void swap_rows(u32x4 &w) {
     w[A] = r[0], w[B] = r[1];
 }
 
-// Fields i and i + 4 of a word as the floats (16 + u) / 16 of the type; `one` is two floats 1, with their top
-// mantissa bit set where the fields are signed (which flips the field's sign bit: u is the value plus 8).
-template <class X, int I>
-__device__ __forceinline__ uint32_t field_pair(uint32_t w, uint32_t one) {
-    constexpr int kAt = std::is_same_v<X, half_t> ? 6 : 3;   // lowest of the top four mantissa bits
-    constexpr int kShift = kAt - 4 * I;
-    const uint32_t t = kShift >= 0 ? w << (kShift >= 0 ? kShift : 0) : w >> (kShift < 0 ? -kShift : 0);
-    return (t & (0x000f000fu << kAt)) ^ one;
-}
-
 template <class X, bool SIGNED, int PER, int TT, int NW, int MT>
 __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupProduct p, int words, int groups,
                                                                          bool buffered, bool whole_zeros) {
@@ -54,9 +43,6 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
     constexpr int kTokens = 16 * TT, kRows = 16 * MT;
     constexpr int NR = NW * MT;   // 16-row sets: set r is rows r % MT * 16 .. of matrix r / MT
     using H = std::conditional_t<std::is_same_v<X, half_t>, half_t, bf16_t>;
-    constexpr uint32_t kOnes = std::is_same_v<H, half_t> ? 0x3c003c00u : 0x3f803f80u;
-    constexpr uint32_t kField = std::is_same_v<H, half_t> ? (SIGNED ? 0x3e003e00u : 0x3c003c00u)
-                                                          : (SIGNED ? 0x3fc03fc0u : 0x3f803f80u);
     constexpr int kPart = NR * TT * 4;   // sums of a lane
     __shared__ float meet[kNarrowWaves * kPart * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -168,7 +154,10 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
             for (int a = 0; a < NR; ++a) by_instruction(words_of[a] = f.w[a]);
 #pragma unroll
             for (int c = 0; c < kGroups; ++c) {
-                f32x4 part[NR][TT] = {}, sum[TT] = {};
+                f32x4 part[NR][TT] = {};
+                ZeroPoint z[NR];
+#pragma unroll
+                for (int a = 0; a < NR; ++a) z[a] = zero_point<SIGNED>(SIGNED ? 0u : (f.z[a] >> (8 * c)) & 255u);
 #pragma unroll
                 for (int b = 0; b < PER; ++b) {
                     const int i = c * PER + b;
@@ -179,16 +168,9 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                         if (BUF && step * 128 + 128 > p.K) clear_behind(r, p.K - k_of(step, i));
                         x_operand_paired(r, x[t]);
                     }
-                    const u32x4 ones = {kOnes, kOnes, kOnes, kOnes};
-#pragma unroll
-                    for (int t = 0; t < TT; ++t)
-#pragma unroll
-                        for (int j = 0; j < kPieces<X>; ++j) sum[t] = mfma<H>(x[t][j], ones, sum[t]);
 #pragma unroll
                     for (int a = 0; a < NR; ++a) {
-                        const uint32_t w = words_of[a][i];
-                        const u32x4 v = {field_pair<H, 0>(w, kField), field_pair<H, 1>(w, kField), field_pair<H, 2>(w, kField),
-                                         field_pair<H, 3>(w, kField)};
+                        const u32x4 v = whole_operand<H, SIGNED>(words_of[a][i], z[a]);
 #pragma unroll
                         for (int t = 0; t < TT; ++t)
 #pragma unroll
@@ -197,15 +179,11 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
                 }
                 if (kGroups > 1 && step * kGroups + c >= groups) break;   // behind the row's last group
 #pragma unroll
-                for (int a = 0; a < NR; ++a) {
-                    const float z = SIGNED ? 8.0f : (float)((f.z[a] >> (8 * c)) & 255u);
-                    const float zz = fmaf(z, -0.0625f, -1.0f), s = 16.0f * f.s[a][c];
+                for (int a = 0; a < NR; ++a)
 #pragma unroll
                     for (int t = 0; t < TT; ++t)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            acc[a][t][r] = fmaf(s, fmaf(zz, sum[t][r], part[a][t][r]), acc[a][t][r]);
-                }
+                        for (int r = 0; r < 4; ++r) acc[a][t][r] = fmaf(f.s[a][c], part[a][t][r], acc[a][t][r]);
             }
         };
         Step f0, f1;

@@ -116,3 +116,16 @@ def product_is_the_formulas(typ, T, K, M=70):
 @pytest.mark.parametrize("T", [1, 2])
 def test_products_of_one_and_two_tokens(typ, T, K):
     product_is_the_formulas(typ, T, K)
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("K", [256, 2051, 4100])
+@pytest.mark.parametrize("T", [3, 16, 20, 70, 300])
+def test_products_of_more_tokens(typ, T, K):
+    product_is_the_formulas(typ, T, K)
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_wide_products_of_few_tokens(typ):
+    """So many rows that a workgroup takes 32 of them."""
+    product_is_the_formulas(typ, 5, 260, 8200)
