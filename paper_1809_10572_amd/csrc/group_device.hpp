@@ -152,6 +152,12 @@ __device__ __forceinline__ ZeroPoint zero_point(uint32_t z) {   // of 0 .. 255
     const half2_t k960 = {(half_t)960.0f, (half_t)960.0f};
     return {-at1024, k960 - at1024};
 }
+// -(1024 + z) and -(64 + z) in one word.
+template <bool SIGNED>
+__device__ __forceinline__ float zero_point_word(uint32_t z) {
+    const ZeroPoint p = zero_point<SIGNED>(z);
+    return __uint_as_float(__builtin_bit_cast(uint32_t, half2_t{p.less[0], p.less16[0]}));
+}
 // The fields as such, put under bits: 1024 + u in [0] and [2], 1024 + 16 u in [1] and [3].
 template <bool SIGNED>
 __device__ __forceinline__ void field_pairs(uint32_t w, half2_t (&out)[4]) {

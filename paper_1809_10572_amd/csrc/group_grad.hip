@@ -2,9 +2,11 @@
 //
 // The sum runs over the rows of W, and a group's scale differs from row to row, so it is part of the summed product
 // and has to be multiplied into an operand in 32-bit floats, one of two ways:
-//   into the weights   s (u - z) as one bf16, rounded, for bf16 (off by at most 2^-8 of each weight, as the types of dy
-//                      and dx are); f16 as two bf16 of together 16 bits and more, dy as two that hold its 11 bits,
-//                      three instructions a product; f32 as three, as is dy, the six largest of their products
+//   into the weights   s (u - z), rounded once to 32 bits, then: for bf16 rounded to one bf16 (off by at most 2^-8 of each
+//                      weight, as the types of dy and dx are); for f16 two bf16 (cut off at 8 bits, the rest rounded), dy as
+//                      two that hold its 11 bits, three instructions a product, the lower parts' left out (in all at most
+//                      9/8 2^-14 of each product, where the result's own rounding is 2^-11); for f32 three, as is dy, the
+//                      six largest of their products (the others at most 2^-21 of each, about 2^-24 as a rule)
 //   into dy            s dy for each group of the tile's columns, as two bf16 (f16, 16 bits and more) or three (f32, all 24);
 //                      u - z is a whole number, exact as one bf16: two or three instructions, but dy is converted
 //                      once for each group, 64 columns at most.  Groups of 64 and 128, and few tokens in f32: 512 x
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     struct Buffers {
         u32x4 x[2][DY][P][BT * 8], w[2][PW][BN * 8];
         u32x4 q[2][kGemmStep * WORDS / 4];        // words as they are stored, 64 rows
-        f32x2 s[2][GROUPS * kScaleRow];           // scales, and zero points (times scales where those go into the weights)
+        f32x2 s[2][GROUPS * kScaleRow];           // scales, and -(1024 + z) and -(64 + z) as two f16
     };
     static_assert((KS - 1) * BT * BN * 4 <= (int)sizeof(Buffers) * KS, "the slices' sums meet in the buffers");
     __shared__ Buffers all[KS];
@@ -105,7 +107,6 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
 
     // Position n of a slice is a step of both pairs' rows; those behind the last are zeros.
     auto step_of = [&](int n) { return __builtin_amdgcn_readfirstlane(2 * slice + n / 2 * 2 * KS + n % 2); };
-    constexpr uint32_t kFlip = SIGNED ? 0x88888888u : 0u;
 
     // On the way in, a thread takes four neighbouring words of a row and the scale of a row and group.
     constexpr int UNITS = kGemmStep * WORDS / 4;
@@ -142,26 +143,32 @@ __global__ __launch_bounds__(64 * TW * MW * KS) void group_grad_kernel(GroupGrad
     auto scale_at = [&](int c, int j, int group) SAMD_INLINE { return group * kScaleRow + j * 8 + c; };
     auto store_words = [&](int buf) SAMD_INLINE {
         all[slice].q[buf][four_at(urow / 8, urow % 8, ucol)] = fw.q;
-        all[slice].s[buf][scale_at(srow / 8, srow % 8, sgroup)] = f32x2{fw.s, (GX ? 1.0f : fw.s) * (SIGNED ? 8.0f : (float)fw.z)};
+        all[slice].s[buf][scale_at(srow / 8, srow % 8, sgroup)] = f32x2{fw.s, zero_point_word<SIGNED>(fw.z)};
     };
     // On to the operands, a thread takes KPT columns of 8 rows; eight neighbouring threads different rows.
     const int chunk = tid % 8, column = (tid / 8 % WORDS) * 8 + tid % DECODERS / BN * KPT;
     const int word = column / 8, shift = column % 8 * 4, sgroup_of = column >> gshift;
+    // four fields: the bytes that hold them into the lower bytes of two halves
+    const uint32_t spread = shift ? 0x0c030c02u : 0x0c010c00u;
     auto decode = [&](int buf) SAMD_INLINE {
         if (DECODERS < THREADS && tid >= DECODERS) return;
+        const uint32_t one = as_is(SIGNED ? 0x64086408u : 0x64006400u), sixteen = SIGNED ? as_is(0x64806480u) : one;
+        const float unit = as_float(1.0f);
         float v[KPT][8];
         const uint32_t *q = (const uint32_t *)all[slice].q[buf];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t w = q[four_at(chunk, j, word / 4) * 4 + word % 4];
             const f32x2 s = all[slice].s[buf][scale_at(chunk, j, sgroup_of)];
-            const uint32_t u = ((w ^ kFlip) >> shift) & (KPT == 4 ? 0xffffu : 0xffu);
-            const uint32_t lo = as_is(u & 0x0f0f0f0fu), hi = as_is((u >> 4) & 0x0f0f0f0fu);
+            // u - z exactly, by a multiply-add on the f16 1024 + u or 1024 + 16 u; times its scale that is rounded once
+            const half2_t less = __builtin_bit_cast(half2_t, __float_as_uint(s[1]));
+            const uint32_t u = KPT == 4 ? __builtin_amdgcn_perm(0u, w, spread) : w >> shift;
+            const half2_t even = __builtin_bit_cast(half2_t, (u & 0x000f000fu) ^ one);
+            const half2_t odd = __builtin_bit_cast(half2_t, (u & 0x00f000f0u) ^ sixteen);
 #pragma unroll
             for (int c = 0; c < KPT; c += 2) {
-                const float l = (float)((lo >> (4 * c)) & 255u), h = (float)((hi >> (4 * c)) & 255u);
-                v[c][j] = GX ? l - s[1] : fmaf(s[0], l, -s[1]);
-                v[c + 1][j] = GX ? h - s[1] : fmaf(s[0], h, -s[1]);
+                v[c][j] = (GX ? 1.0f : s[0]) * fmaf((float)even[c / 2], unit, (float)less[0]);
+                v[c + 1][j] = (GX ? 1.0f : s[0]) * fmaf((float)odd[c / 2], 0.0625f, (float)less[1]);
             }
         }
 #pragma unroll

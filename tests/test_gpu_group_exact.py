@@ -129,3 +129,31 @@ def test_products_of_more_tokens(typ, T, K):
 def test_wide_products_of_few_tokens(typ):
     """So many rows that a workgroup takes 32 of them."""
     product_is_the_formulas(typ, 5, 260, 8200)
+
+
+# What a product dy w may lose on its way into a gradient, as a part of it.  bf16: the weight rounded to a bf16, 2^-8.
+# f16: both cut to 8 bits, what is cut off below 2^-7 of each (of dy's 11 bits, at most 7/8 of that); the weight's cut-off
+# part is rounded to 8 bits, 2^-8 of at most 2^-8 where it is largest, 2^-16; the product of the cut-off parts is left out,
+# 7/8 2^-14; together 9/8 2^-14.  f32: pieces below 1, 2^-7 and 2^-15 of each, exact; left out are the second by the third,
+# twice, and the third by the third: 2 2^-22 + 2^-30; and the weight's own product with its scale, 2^-24.
+LOST = {"f32": 2.0 ** -21 + 2.0 ** -23, "f16": 1.125 * 2.0 ** -14 + 2.0 ** -23, "bf16": 2.0 ** -8 + 2.0 ** -23}
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(3, 300, 70), (40, 2051, 70), (600, 300, 260), (2040, 200, 4090)])
+def test_gradients_are_the_formulas(typ, size):
+    """Few and many tokens, for every tile of the gradient: nothing from weights that are nothing, and the bound of
+    products with what the products themselves may lose."""
+    T, M, K = size
+    gen = torch.Generator(device=DEV).manual_seed(T + K)
+    dy = torch.exp2(12 * torch.rand(T, M, generator=gen, device=DEV) - 10).to(TYPES[typ])
+    for group in (32, 64, 128):
+        for zero in (None, 3, 15, "any"):
+            w, _ = near_zero_points(gen, M, K, group, zero, 0)
+            assert not samd.group_matmul_grad(dy, w).any(), (group, zero)
+            assert not samd.group_matmul_grad(dy, w, dy, w).any(), (group, zero)
+            w, values = near_zero_points(gen, M, K, group, zero, 3)
+            want, size = dy.double() @ values, dy.double() @ values.abs()
+            bound = rounding(typ, want) + (LOST[typ] + (M / 32 + 64) * 2.0 ** -24) * size
+            off = ((samd.group_matmul_grad(dy, w).double() - want).abs() - bound).max().item()
+            assert off <= 0, (group, zero, off)
