@@ -1,12 +1,12 @@
 """Group-scaled rows on the GPU: what a result owes to the formula alone, against 64 bits.  The bounds count a weight as
 its value |s (q - z)|, not as its fields, so that a weight equal to its zero point may not show in a result at all."""
-import numpy as np
+import math
+
 import pytest
 import torch
 
 import paper_1809_10572_amd as samd
 from paper_1809_10572_amd import GroupRows
-import group_reference as ref
 
 pytestmark = pytest.mark.gpu
 TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
@@ -157,3 +157,76 @@ def test_gradients_are_the_formulas(typ, size):
             bound = rounding(typ, want) + (LOST[typ] + (M / 32 + 64) * 2.0 ** -24) * size
             off = ((samd.group_matmul_grad(dy, w).double() - want).abs() - bound).max().item()
             assert off <= 0, (group, zero, off)
+
+
+# ---- the activations' tails -----------------------------------------------------------------------
+
+def activation_of(g, act):
+    """act(g), act'(g) and the terms that the latter is the sum of, in 64 bits and without cancellation."""
+    if act == "silu":
+        e = torch.exp(-g.abs())
+        p, q = torch.where(g < 0, e, 1.0) / (1 + e), torch.where(g < 0, 1.0, e) / (1 + e)   # p(g) and p(-g) = 1 - p(g)
+        return g * p, (p, p * g * q)
+    p = 0.5 * torch.special.erfc(-g * math.sqrt(0.5))
+    return g * p, (p, g * torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi))
+
+
+def activation_bounds(g, act):
+    """What 32-bit arithmetic may lose of act(g) and of act'(g).  gelu: the argument g / sqrt 2 is off by 1.5 2^-24 of
+    itself, its constant and its product, which erfc turns into g^2 + 1 times as much at most; erfc itself by 16 last places, 32
+    units of 2^-24; two products.  Its density: g^2 / 2 off by 2^-24 of itself, which the exponential turns into as much,
+    the exponential by 2 last places, three products."""
+    value, (p, rest) = activation_of(g, act)
+    assert act == "gelu"
+    rel, rel_rest = 1.5 * (g * g + 1) + 36, 0.5 * g * g + 10
+    unit = 2.0 ** -24
+    return value, value.abs() * rel * unit, p + rest, (p.abs() * rel + rest.abs() * rel_rest + (p + rest).abs()) * unit
+
+
+def one_hot_rows(gen, at, M):
+    """M rows of 32 weights that are 0 but for a 1 at k = at, of scale 1."""
+    q = torch.zeros(M, 32, dtype=torch.long, device=DEV)
+    q[:, at] = 1
+    return from_fields(gen, q, 32, None, torch.ones(M, 1, device=DEV))[0]
+
+
+def tail_of_gated(typ, act, g):
+    """h = act(g) u for given g and u = 512, tokens enough for each kernel; and the stored form's h."""
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    want, off, _, _ = activation_bounds(g, act)
+    want, off = 512 * want, 512 * off
+    bound = rounding(typ, want) + off + 2.0 ** -24 * want.abs()
+    for M in (1, 5):
+        wg, wu = one_hot_rows(gen, 0, M), one_hot_rows(gen, 1, M)
+        for T in (1, 2, 5, 20, 600):
+            for i in range(0, len(g), T):
+                x = torch.zeros(T, 32, dtype=TYPES[typ], device=DEV)
+                n = min(T, len(g) - i)
+                x[:n, 0], x[:, 1] = g[i:i + n].to(TYPES[typ]), 512
+                for h in (samd.group_gated(x, wg, wu, act), samd.group_gated_save(x, wg, wu, act)[0]):
+                    err = (h[:n].double() - want[i:i + n, None]).abs() - bound[i:i + n, None]
+                    assert err.max() <= 0, (M, T, g[i + err.max(1)[0].argmax()].item())
+
+
+def tail_of_gated_grad(typ, act, g, step):
+    """dg and du for g = -step q in stored form, u = 512, dh = 1."""
+    value, off, slope, off_slope = activation_bounds(g, act)
+    n = len(g)
+    q8 = torch.zeros(n, 4, dtype=torch.int8, device=DEV)
+    q8[:, 0] = (g / step).round().to(torch.int8)
+    u8 = torch.zeros_like(q8)
+    u8[:, 0] = 64
+    g8 = GroupRows(q8.view(torch.int32), torch.full((n, 1), step, device=DEV), None, 1, 8, 32)
+    u8 = GroupRows(u8.view(torch.int32), torch.full((n, 1), 8.0, device=DEV), None, 1, 8, 32)
+    dg, du = samd.group_gated_grad(torch.ones(n, 1, dtype=TYPES[typ], device=DEV), g8, u8, act)
+    err = (dg[:, 0].double() - 512 * slope).abs() - (rounding(typ, 512 * slope) + 512 * off_slope + 2.0 ** -23 * 512 * slope.abs())
+    assert err.max() <= 0, ("dg", g[err.argmax()].item())
+    err = (du[:, 0].double() - value).abs() - (rounding(typ, value) + off + 2.0 ** -24 * value.abs())
+    assert err.max() <= 0, ("du", g[err.argmax()].item())
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_gelu_keeps_its_tail(typ):
+    g = -torch.arange(0, 97, device=DEV).double() / 8   # 0 .. -12, exact in every type
+    tail_of_gated(typ, "gelu", g)
+    tail_of_gated_grad(typ, "gelu", g, 0.125)
