@@ -204,12 +204,13 @@ __device__ __forceinline__ u32x4 whole_operand(uint32_t w, const ZeroPoint &z) {
     return out;
 }
 
-// The gated block's activation: a = act(g), da = act'(g), with the 32-bit exponential and complementary error function.
-// erfc(-g / sqrt 2), not 1 + erf: that cancels for negative g (off by 4 % at -5, 0 from -5.5 on).  What the argument's
-// rounding leaves grows with g^2: 1.5 (g^2 + 1) + 36 units of 2^-24 of the value, the function's own 16 last places in them.
+// The gated block's activation: a = act(g), da = act'(g), with the 32-bit exponential and complementary error function;
+// values next to 0 keep their relative accuracy.  erfc(-g / sqrt 2), not 1 + erf: that cancels for negative g (off by 4 %
+// at -5, 0 from -5.5 on).  What the argument's rounding leaves grows with g^2: 1.5 (g^2 + 1) + 36 units of 2^-24 of the
+// value, 16 last places of the function in them.
 __device__ __forceinline__ void activation(int act, float g, float &a, float &da) {
     if (act == SAMD_ACT_SILU) {
-        const float p = 1.0f / (1.0f + expf(-g));
+        const float e = expf(-fabsf(g)), p = (g < 0.0f ? e : 1.0f) / (1.0f + e);   // e^-g overflows from -88.7 on
         a = g * p;
         da = p * (1.0f + g * (1.0f - p));
     } else {

@@ -175,9 +175,12 @@ def activation_bounds(g, act):
     """What 32-bit arithmetic may lose of act(g) and of act'(g).  gelu: the argument g / sqrt 2 is off by 1.5 2^-24 of
     itself, its constant and its product, which erfc turns into g^2 + 1 times as much at most; erfc itself by 16 last places, 32
     units of 2^-24; two products.  Its density: g^2 / 2 off by 2^-24 of itself, which the exponential turns into as much,
-    the exponential by 2 last places, three products."""
+    the exponential by 2 last places, three products.  silu: the exponential, a sum, a quotient and a product; the slope's
+    p (1 + g (1 - p)) the same for terms of p and p g; the exponential's steps of 2^-149 below 2^-126."""
     value, (p, rest) = activation_of(g, act)
-    assert act == "gelu"
+    if act == "silu":
+        off = 8 * 2.0 ** -24 * p + 2.0 ** -149
+        return value, g.abs() * off, p + rest, (1 + g.abs()) * off
     rel, rel_rest = 1.5 * (g * g + 1) + 36, 0.5 * g * g + 10
     unit = 2.0 ** -24
     return value, value.abs() * rel * unit, p + rest, (p.abs() * rel + rest.abs() * rel_rest + (p + rest).abs()) * unit
@@ -195,7 +198,7 @@ def tail_of_gated(typ, act, g):
     gen = torch.Generator(device=DEV).manual_seed(1)
     want, off, _, _ = activation_bounds(g, act)
     want, off = 512 * want, 512 * off
-    bound = rounding(typ, want) + off + 2.0 ** -24 * want.abs()
+    bound = rounding(typ, want) + off + 2.0 ** -24 * want.abs() + 512 * 2.0 ** -149
     for M in (1, 5):
         wg, wu = one_hot_rows(gen, 0, M), one_hot_rows(gen, 1, M)
         for T in (1, 2, 5, 20, 600):
@@ -230,3 +233,10 @@ def test_gelu_keeps_its_tail(typ):
     g = -torch.arange(0, 97, device=DEV).double() / 8   # 0 .. -12, exact in every type
     tail_of_gated(typ, "gelu", g)
     tail_of_gated_grad(typ, "gelu", g, 0.125)
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_silu_keeps_its_tail(typ):
+    g = 4.0 - torch.arange(0, 105, device=DEV).double()   # 4 .. -100
+    tail_of_gated(typ, "silu", g)
+    tail_of_gated_grad(typ, "silu", g, 1.0)
