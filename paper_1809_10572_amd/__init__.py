@@ -775,6 +775,8 @@ def conv2d_spaced_tune(xp: torch.Tensor, xfmt: Fmt, wp: torch.Tensor, wfmt: Fmt,
 
 
 # --- group-scaled rows (include/samd.h, "Group-scaled rows") ------------------------------
+# These calls record nothing for autograd: a training program calls the gradients itself, from the backward of a
+# torch.autograd.Function or without autograd at all.  A tensor that asks for gradients where they are recorded is refused.
 
 GATED_GROUP = 32
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -812,6 +814,13 @@ def _launch(fn, t: torch.Tensor, *args) -> None:
         _check(status)
 
 
+def _no_record(name: str) -> None:
+    """Refuse a tensor that asks for gradients, unless none are recorded here."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} asks for gradients, which this call does not record: call it under torch.no_grad() (the "
+                         "forward and backward of a torch.autograd.Function are) and take the gradients from the group_*_grad calls")
+
+
 def _matrix(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> Tuple[int, int, int]:
     """(rows, columns, row stride) of a float tensor: contiguous, its leading axes taken as
     rows, or two-dimensional with contiguous rows.  `like`: of that tensor's type and device."""
@@ -821,6 +830,8 @@ def _matrix(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> 
         raise ValueError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
     if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} must have the type and device of the other operands")
+    if t.requires_grad:
+        _no_record(name)
     shape = t.shape
     if not shape:
         raise ValueError(f"{name} must have at least one axis")
@@ -839,6 +850,8 @@ def _group_rows(r: GroupRows, name: str, like: torch.Tensor) -> int:
         raise ValueError(f"{name}: groups of 32, 64 or 128 values of 4 or 8 bits")
     words, groups = -(-cols * bits // 32), -(-cols // group)
     at = like.get_device()
+    if scale.requires_grad:
+        _no_record(f"{name}.scale")
     # one condition for what is right, for calls that last some microseconds; then what is wrong
     if (at >= 0 and q.dtype is torch.int32 and scale.dtype is torch.float32 and q.get_device() == at
             and scale.get_device() == at and q.is_contiguous() and scale.is_contiguous() and words and q.shape
@@ -868,6 +881,11 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+# Tells autograd that a tensor given for a result changes, as torch's own operations do: a graph that saved its values
+# refuses to go backward from them.
+_written = torch.autograd.graph.increment_version
+
+
 def _out_matrix(out: Optional[torch.Tensor], shape, like: torch.Tensor, name: str = "out") -> Tuple[torch.Tensor, int]:
     """The result tensor and its row stride."""
     if out is None:
@@ -878,6 +896,7 @@ def _out_matrix(out: Optional[torch.Tensor], shape, like: torch.Tensor, name: st
         want *= n
     if cols != shape[-1] or (cols and rows != want):
         raise ValueError(f"{name} must hold {want} rows of {shape[-1]} values")
+    _written(out)
     return out, ld
 
 
@@ -913,6 +932,7 @@ def group_dequantize(r: GroupRows, dtype: torch.dtype = torch.float32, out: Opti
         orows, ocols, ld = _matrix(out, "out")
         if ocols != r.cols or (r.cols and orows != rows) or out.get_device() != r.q.get_device():
             raise ValueError(f"out must hold {rows} rows of {r.cols} values on the device of r")
+        _written(out)
     _launch(lib().samd_group_dequantize, r.q, r.q.data_ptr(), r.scale.data_ptr(), _ptr(r.zero), rows, r.cols,
             _FMTS[r.bits, r.zero is None], r.group, out.data_ptr(), _TYPES[out.dtype], ld)
     return out
