@@ -886,8 +886,45 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 _written = torch.autograd.graph.increment_version
 
 
-def _out_matrix(out: Optional[torch.Tensor], shape, like: torch.Tensor, name: str = "out") -> Tuple[torch.Tensor, int]:
-    """The result tensor and its row stride."""
+def _extent(t: torch.Tensor) -> Tuple[int, int, int, int]:
+    """(address, rows, bytes of a row, bytes from row to row) of what a checked tensor covers."""
+    size = t.element_size()
+    if t.is_contiguous():
+        return t.data_ptr(), 1, t.numel() * size, t.numel() * size
+    return t.data_ptr(), t.shape[0], t.shape[1] * size, t.stride(0) * size
+
+
+def _meet(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two checked tensors have a byte in common.  Rows of one buffer may lie between those of the other."""
+    return _rows_meet(_extent(a), _extent(b))
+
+
+def _rows_meet(a, b) -> bool:
+    (p, n, row, step), (q, m, width, far) = (a, b) if a[1] <= b[1] else (b, a)
+    if p >= q + (m - 1) * far + width or q >= p + (n - 1) * step + row or not (row and width):
+        return False
+    if step == far:   # rows i and j = i + k meet where the latter starts less than a row before or behind
+        k = max(-((q - p + width - 1) // far), 1 - n)
+        return k < m and k * far + q - p < row
+    for at in range(p, p + n * step, step):   # the first row that ends behind this one's start
+        j = max((at - q - width) // far + 1, 0)
+        if j < m and q + j * far < at + row:
+            return True
+    return False
+
+
+def _check_apart(name: str, out: torch.Tensor, *others) -> None:
+    """A result given by the caller shares no memory with the call's other tensors."""
+    extent = _extent(out)
+    end = extent[0] + (extent[1] - 1) * extent[3] + extent[2]
+    for o in others:
+        for t in o[:3] if type(o) is GroupRows else (o,):
+            if t is not None and t.data_ptr() < end and _rows_meet(extent, _extent(t)):
+                raise ValueError(f"{name} overlaps another operand of the call")
+
+
+def _out_matrix(out: Optional[torch.Tensor], shape, like: torch.Tensor, *others, name: str = "out") -> Tuple[torch.Tensor, int]:
+    """The result tensor and its row stride; one that is given may not overlap `like` and the others."""
     if out is None:
         return like.new_empty(shape), shape[-1]
     rows, cols, ld = _matrix(out, name, like)
@@ -896,6 +933,7 @@ def _out_matrix(out: Optional[torch.Tensor], shape, like: torch.Tensor, name: st
         want *= n
     if cols != shape[-1] or (cols and rows != want):
         raise ValueError(f"{name} must hold {want} rows of {shape[-1]} values")
+    _check_apart(name, out, like, *others)
     _written(out)
     return out, ld
 
@@ -932,6 +970,7 @@ def group_dequantize(r: GroupRows, dtype: torch.dtype = torch.float32, out: Opti
         orows, ocols, ld = _matrix(out, "out")
         if ocols != r.cols or (r.cols and orows != rows) or out.get_device() != r.q.get_device():
             raise ValueError(f"out must hold {rows} rows of {r.cols} values on the device of r")
+        _check_apart("out", out, r)
         _written(out)
     _launch(lib().samd_group_dequantize, r.q, r.q.data_ptr(), r.scale.data_ptr(), _ptr(r.zero), rows, r.cols,
             _FMTS[r.bits, r.zero is None], r.group, out.data_ptr(), _TYPES[out.dtype], ld)
@@ -958,7 +997,7 @@ def group_matmul(x: torch.Tensor, w: GroupRows, out: Optional[torch.Tensor] = No
     """x W^T for x (..., K) and M 4-bit weight rows of K values; one token or many."""
     T, K, ldx = _matrix(x, "x")
     M = _weights(w, "w", x, None, K)
-    out, ldy = _out_matrix(out, x.shape[:-1] + (M,), x)
+    out, ldy = _out_matrix(out, x.shape[:-1] + (M,), x, w)
     _launch(lib().samd_group_matmul, x, x.data_ptr(), _TYPES[x.dtype], ldx, w.q.data_ptr(), w.scale.data_ptr(), _ptr(w.zero),
             _FMTS[4, w.zero is None], w.group, T, M, K, out.data_ptr(), ldy)
     return out
@@ -978,7 +1017,7 @@ def group_matmul_grad(dy: torch.Tensor, w: GroupRows, dy2: Optional[torch.Tensor
             raise ValueError("dy2 must have the sizes and row stride of dy")
         _weights(w2, "w2", dy, M, K)
         _same_kind(w, w2)
-    out, ldx = _out_matrix(out, dy.shape[:-1] + (K,), dy)
+    out, ldx = _out_matrix(out, dy.shape[:-1] + (K,), dy, w, dy2, w2)
     second = (None,) * 4 if w2 is None else (dy2.data_ptr(), w2.q.data_ptr(), w2.scale.data_ptr(), _ptr(w2.zero))
     _launch(lib().samd_group_matmul_grad, dy, dy.data_ptr(), _TYPES[dy.dtype], ld, w.q.data_ptr(), w.scale.data_ptr(),
             _ptr(w.zero), *second, _FMTS[4, w.zero is None], w.group, T, M, K, out.data_ptr(), ldx)
@@ -992,7 +1031,7 @@ def _gated(x: torch.Tensor, wg: GroupRows, wu: GroupRows, act: str, out: Optiona
     _weights(wu, "wu", x, M, K)
     _same_kind(wg, wu)
     lead = x.shape[:-1]
-    out, ldh = _out_matrix(out, lead + (M,), x)
+    out, ldh = _out_matrix(out, lead + (M,), x, wg, wu)
     g = u = None
     stored = (None,) * 4
     if save:
@@ -1030,8 +1069,8 @@ def group_gated_grad(dh: torch.Tensor, g: GroupRows, u: GroupRows, act: str = "s
         n = _group_rows(r, name, dh)
         if r.bits != 8 or r.zero is not None or r.cols != M or (M and n != T) or r.group != g.group:
             raise ValueError(f"{name} must hold {T} signed 8-bit rows of {M} values")
-    dg, ldd = _out_matrix(None if out is None else out[0], dh.shape, dh, "dg")
-    du, ldu = _out_matrix(None if out is None else out[1], dh.shape, dh, "du")
+    dg, ldd = _out_matrix(None if out is None else out[0], dh.shape, dh, g, u, name="dg")
+    du, ldu = _out_matrix(None if out is None else out[1], dh.shape, dh, g, u, dg if out else None, name="du")
     if ldu != ldd:
         raise ValueError("dg and du must have one row stride")
     _launch(lib().samd_group_gated_grad, dh, dh.data_ptr(), _TYPES[dh.dtype], ldh, g.q.data_ptr(), g.scale.data_ptr(),
