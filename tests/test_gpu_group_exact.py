@@ -240,3 +240,75 @@ def test_silu_keeps_its_tail(typ):
     g = 4.0 - torch.arange(0, 105, device=DEV).double()   # 4 .. -100
     tail_of_gated(typ, "silu", g)
     tail_of_gated_grad(typ, "silu", g, 1.0)
+
+
+# ---- f32 keeps 24 bits ----------------------------------------------------------------------------
+
+def relative(got, want):
+    return ((got.double() - want).norm() / want.norm()).item()
+
+
+# As test_group_precision shows for the CPU, operands cut to 16 bits put a whole result off by some 200 units of 2^-24 of its
+# norm; sums of K products in 32-bit floats, if each of the K (and three times as many pieces) were rounded alone, by
+# 0.58 sqrt(3 K / 2) at most on average: 47 for K = 4400.  The border lies between.
+KEPT = 2.0 ** -18
+
+# tokens, rows, columns, each tile of the products (rows of the result, summed columns) and of the gradient (summed rows)
+PRECISE = [(1, 500, 4400), (2, 300, 2051), (3, 70, 2304), (16, 500, 1024), (20, 300, 4100), (70, 1013, 2051), (128, 128, 128),
+           (300, 1100, 700), (510, 2000, 1100), (1000, 2100, 1096), (2040, 4090, 576), (2048, 4096, 1330)]
+
+
+@pytest.mark.parametrize("size", PRECISE)
+def test_f32_keeps_24_bits(size):
+    T, M, K = size
+    gen = torch.Generator(device=DEV).manual_seed(T + M)
+    for group in (32, 64, 128):
+        for signed in (True, False):
+            w, values = weights(gen, M, K, group, signed)
+            x, xv = matrix(gen, T, K, "f32")
+            want = xv @ values.t()
+            assert relative(samd.group_matmul(x, w), want) <= KEPT, (group, signed)
+            v, other = weights(gen, M, K, group, signed)
+            u = xv @ other.t()
+            h = want / (1 + torch.exp(-want)) * u
+            # three results of the kind, each off by as much at most, the activation's slope at most 1.1
+            assert relative(samd.group_gated(x, w, v), h) <= 3.3 * KEPT, (group, signed)
+            assert relative(samd.group_gated_save(x, w, v)[0], h) <= 3.3 * KEPT, (group, signed)
+            # sums over K rows, as deep as the products' are
+            w, values = weights(gen, K, M, group, signed)
+            v, other = weights(gen, K, M, group, signed)
+            dy, dyv = matrix(gen, T, K, "f32")
+            want = dyv @ values
+            assert relative(samd.group_matmul_grad(dy, w), want) <= KEPT, (group, signed)
+            assert relative(samd.group_matmul_grad(dy, w, x, v), want + xv @ other) <= KEPT, (group, signed)
+
+
+# ---- projections that cannot be stored ------------------------------------------------------------
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T", [4, 70, 600])
+def test_stored_rows_of_nothing_and_of_no_number(typ, T):
+    """A token of zeros is stored as zeros of scale 0, one with an infinity or a NaN as words of 0 and scales of NaN; the
+    other tokens as without them."""
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    for M, K, group in ((45, 90, 32), (700, 256, 128)):
+        wg, wu = weights(gen, M, K, group, False)[0], weights(gen, M, K, group, False)[0]
+        x, _ = matrix(gen, T, K, typ)
+        x[0] = 0
+        h, g, u = samd.group_gated_save(x, wg, wu)
+        assert not h[0].any()
+        for r in (g, u):
+            assert not r.q[0].any() and not r.scale[0].any() and (r.scale[1:] > 0).all()
+        bad = {1: float("inf"), T // 2: float("nan"), T - 1: float("-inf")}
+        for t, v in bad.items():
+            x[t, t % K] = v
+        h2, g2, u2 = samd.group_gated_save(x, wg, wu)
+        rest = torch.tensor([t not in bad for t in range(T)], device=DEV)
+        assert torch.equal(h2[rest], h[rest]) and not torch.isfinite(h2[~rest]).any()
+        for r, r2 in ((g, g2), (u, u2)):
+            assert torch.equal(r2.q[rest], r.q[rest]) and torch.equal(r2.scale[rest], r.scale[rest])
+            assert not r2.q[~rest].any() and torch.isnan(r2.scale[~rest]).all()
+            assert torch.isnan(samd.group_dequantize(r2)[~rest]).all()
+        dg, du = samd.group_gated_grad(torch.ones_like(h2), g2, u2)
+        assert torch.isnan(dg[~rest]).all() and torch.isnan(du[~rest]).all()
+        assert torch.isfinite(dg[rest]).all() and torch.isfinite(du[rest]).all()
