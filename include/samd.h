@@ -521,14 +521,20 @@ int samd_scale(const uint32_t *a, int64_t nwords, samd_fmt f, int32_t scalar, ui
  * (zero 0 when signed).  All three are dense.
  *
  * Float tensors are row-major with a row stride in elements (`ld...`, at least the row's
- * length; what lies between a row's end and the next row is neither read nor written) and
- * an element type.  They must be aligned to their element (SAMD_EALIGN); rows that all
- * start on 16 bytes are read and written fastest.  Sums and scales are 32-bit floats
- * whatever the type; a result is rounded once, to the type, unless a call says more.
- * Sizes are at most 2^31 - 1 each (K, a row of weights, and M of samd_group_matmul_grad at
- * most 2^25, and a result of so many values that its launch would need 2^32 threads, some
- * 10^8 rows of weights for a token: SAMD_EUNSUPPORTED), offsets are 64-bit.  Inputs and
- * outputs must not overlap.
+ * length) and an element type.  What lies between a result's rows is not written; what lies
+ * between an input's rows has no part in a result, but may be read.  Tensors must be
+ * aligned to their element (SAMD_EALIGN); rows that all start on 16 bytes are read and
+ * written fastest, and products of many tokens with 16-bit rows that do not all start on 4
+ * bytes (an odd K or stride; in the gradient an odd M) take about twice as long.
+ * Sums and scales are 32-bit floats whatever the type; a result is rounded once, to the
+ * type.  A field less its zero point is exact in every call: a weight equal to its zero
+ * point adds nothing.  samd_group_matmul and samd_group_gated multiply exactly (f32 values
+ * on the matrix cores down to 2^-133: all 24 bits from 2^-110 on); what
+ * samd_group_matmul_grad may lose is said there.
+ * Sizes are at most 2^31 - 1 each, K of the products and M of samd_group_matmul_grad at
+ * least 1 (K, a row of weights, and M of samd_group_matmul_grad at most 2^25, and a result
+ * of so many values that its launch would need 2^32 threads, some 10^8 rows of weights for
+ * a token: SAMD_EUNSUPPORTED), offsets are 64-bit.  Inputs and outputs must not overlap.
  * No call needs a workspace, and a call's results do not depend on what else runs: no
  * atomics, a fixed order of every sum. */
 enum { SAMD_F32 = 0, SAMD_F16 = 1, SAMD_BF16 = 2 };
@@ -563,7 +569,11 @@ int samd_group_matmul(const void *x, int32_t type, int64_t ldx, const uint32_t *
  * wf is unsigned), dx = dy W + dy2 W2, both sums before the one rounding: the input
  * gradient of samd_group_gated.  dy and dy2 have the same row stride.  A dy row that holds an
  * infinity, a NaN or a magnitude that exceeds 2^100 itself or times a scale may give a dx row
- * of NaN and infinities, as above. */
+ * of NaN and infinities, as above.
+ * The scales belong to the summed rows, so they are multiplied into an operand and rounded
+ * with it: bf16 rounds each weight to a bf16, by at most 2^-8 of it, as its dy and dx are
+ * rounded (a second piece would double the matrix work); f16 loses at most 9/8 2^-14 of a
+ * product, f32 2^-21 and about 2^-24 as a rule. */
 int samd_group_matmul_grad(const void *dy, int32_t type, int64_t lddy, const uint32_t *q, const float *scale,
                            const uint8_t *zero, const void *dy2, const uint32_t *q2, const float *scale2,
                            const uint8_t *zero2, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K,

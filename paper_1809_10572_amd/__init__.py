@@ -1006,7 +1006,7 @@ def group_matmul(x: torch.Tensor, w: GroupRows, out: Optional[torch.Tensor] = No
 def group_matmul_grad(dy: torch.Tensor, w: GroupRows, dy2: Optional[torch.Tensor] = None, w2: Optional[GroupRows] = None,
                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dy W (+ dy2 W2): the gradient of group_matmul (or, with both pairs, of group_gated's
-    two products) with respect to x."""
+    two products) with respect to x.  bfloat16 rounds the weights to bfloat16 on the way."""
     T, M, ld = _matrix(dy, "dy")
     K = w.cols
     _weights(w, "w", dy, M, None)
