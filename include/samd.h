@@ -525,7 +525,7 @@ int samd_scale(const uint32_t *a, int64_t nwords, samd_fmt f, int32_t scalar, ui
  * between an input's rows has no part in a result, but may be read.  Tensors must be
  * aligned to their element (SAMD_EALIGN); rows that all start on 16 bytes are read and
  * written fastest, and products of many tokens with 16-bit rows that do not all start on 4
- * bytes (an odd K or stride; in the gradient an odd M) take about twice as long.
+ * bytes (an odd K or stride; in the gradient an odd M) take two to three times as long.
  * Sums and scales are 32-bit floats whatever the type; a result is rounded once, to the
  * type.  A field less its zero point is exact in every call: a weight equal to its zero
  * point adds nothing.  samd_group_matmul and samd_group_gated multiply exactly (f32 values
