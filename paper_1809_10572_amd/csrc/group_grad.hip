@@ -10,7 +10,7 @@
 //   into dy            s dy for each group of the tile's columns, as two bf16 (f16, 16 bits and more) or three (f32, all 24);
 //                      u - z is a whole number, exact as one bf16: two or three instructions, but dy is converted
 //                      once for each group, 64 columns at most.  Groups of 64 and 128, and few tokens in f32: 512 x
-//                      4096 x 4096 f32 113 us to 90; with groups of 32 2048 tokens take 687 us so and 462 the other way
+//                      4096 x 4096 f32 113 us to 91; with groups of 32 2048 tokens take 687 us so and 467 the other way
 // (a bf16 holds any float's range; an f16 operand would lose small scales).  Everything is summed in 32-bit floats, both
 // pairs into one sum, and rounded once.
 //
@@ -21,8 +21,8 @@
 // thread then takes the same KPT columns of eight rows and writes KPT operand parts of eight rows each, so that
 // the transposition costs nothing but its choice of pairs.
 //
-// Measured (graph of calls, 4096 x 4096 weights, signed groups of 128): 2048 tokens bf16 91 us (757 TFLOP/s of the
-// 1150 that a large library product reaches), f32 353 us, 1024 tokens f16 108 us; 128 tokens bf16 29 us, f16 35, f32 39.
+// Measured (graph of calls, 4096 x 4096 weights, signed groups of 128): 2048 tokens bf16 92 us (745 TFLOP/s of the
+// 1150 that a large library product reaches), f32 355 us, 1024 tokens f16 105 us; 128 tokens bf16 28 us, f16 33, f32 36.
 // Bound by what lies between two barriers of a step (operands out of LDS, the next step's decoding and writes), only in
 // part under the other waves' products.  Few tokens are bound by the chain of steps of a workgroup, whose number only
 // the slices cut: as many as LDS holds.
@@ -330,8 +330,9 @@ int launch_grad_tile(const GroupGrad &p, hipStream_t s) {
     return check_launch("samd_group_matmul_grad");
 }
 
-// A workgroup fills a CU, so a tile costs its time for each round of 256 workgroups; the units are microseconds measured
-// for M = 4096 (they grow with M alike).
+// A workgroup fills a CU, so a tile costs its time for each round of 256 workgroups; the units are about the microseconds
+// measured for M = 4096 (they grow with M alike).  Rows of dy at odd addresses, an odd M of a 16-bit type, have the smallest
+// tile alone: 2048 x 4095 x 4096 bf16 takes 309 us where 4096 takes 92, 1024 tokens f16 208 and 105.
 template <class X>
 int launch_grad_of(const GroupGrad &p, hipStream_t s) {
     const int64_t rows = std::min<int64_t>(p.T, 256);

@@ -13,8 +13,9 @@
 // A workgroup computes 16 MT rows of W for 16 TT tokens, its eight waves taking steps of K in turn; their
 // sums meet in LDS in a fixed order.
 //
-// Bound by what each CU reads of x through L1 and by the latency of a wave's few steps: 16 x 4096 x 4096 bf16 takes 8.5 us
-// (signed groups of 128), 16 x 8192 x 8192 22 us, against 1.8 and 7 for reading the weights once at 5.2 TB/s.
+// Bound by the latency of a wave's few steps and by what each CU reads through L1: 16 x 4096 x 4096 bf16 takes 8.5 us
+// (signed groups of 128), 16 x 8192 x 8192 22 us, against 1.8 and 7 for reading the weights once at 5.2 TB/s.  (f16, unsigned
+// groups of 64, 4096 x 4096, counted: half of the waves' cycles are waits, 15400 accesses of a CU's L1 in some 21000 cycles.)
 #pragma once
 
 #include "group_vector.hpp"
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void group_narrow_kernel(GroupPr
 }
 
 // Launches the kernel: 16 tokens a workgroup, or 32; 16 rows of W, or, where those are two workgroups and more for each
-// CU, 32, which read x half as often (16 x 8192 x 8192, unsigned groups of 64: 28.8 us with 16 rows, 22.0 with 32;
+// CU, 32, which read x half as often (16 x 8192 x 8192, unsigned groups of 64: 29.0 us with 16 rows, 22.0 with 32;
 // 16 x 4096 x 4096: 9.7 and 12.9).  The gated block's two matrices share x already: 32 rows of each are slower always.
 template <class X, bool SIGNED, int NW>
 int launch_narrow(const GroupProduct &p, int words, int groups, hipStream_t s) {

@@ -163,7 +163,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void group_vector_kernel(GroupProdu
 
 // Launches the kernel for p.T tokens (1 or 2).  Two rows a wave, so that x is read from LDS half as
 // often, unless that leaves CUs without a workgroup (1024 x 16384 weights: 7.4 us with one row a wave,
-// 9.5 with two; 16384 x 8192: 17.7 and 14.8).
+// 9.6 with two; 16384 x 8192: 21.7 and 17.2).
 template <class X, bool SIGNED, int NW>
 int launch_vector(const GroupProduct &p, int words, int groups, int gshift, hipStream_t s) {
     const int steps = (words + 255) / 256;
