@@ -918,7 +918,7 @@ def _check_apart(name: str, out: torch.Tensor, *others) -> None:
     extent = _extent(out)
     end = extent[0] + (extent[1] - 1) * extent[3] + extent[2]
     for o in others:
-        for t in o[:3] if type(o) is GroupRows else (o,):
+        for t in o[:3] if isinstance(o, GroupRows) else (o,):
             if t is not None and t.data_ptr() < end and _rows_meet(extent, _extent(t)):
                 raise ValueError(f"{name} overlaps another operand of the call")
 
