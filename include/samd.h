@@ -573,7 +573,8 @@ int samd_group_matmul(const void *x, int32_t type, int64_t ldx, const uint32_t *
  * The scales belong to the summed rows, so they are multiplied into an operand and rounded
  * with it: bf16 rounds each weight to a bf16, by at most 2^-8 of it, as its dy and dx are
  * rounded (a second piece would double the matrix work); f16 loses at most 9/8 2^-14 of a
- * product, f32 2^-21 and about 2^-24 as a rule. */
+ * product, f32 2^-21 and about 2^-24 as a rule; and of any of them what lies below 2^-133
+ * of a dy, of a weight or of a scaled dy. */
 int samd_group_matmul_grad(const void *dy, int32_t type, int64_t lddy, const uint32_t *q, const float *scale,
                            const uint8_t *zero, const void *dy2, const uint32_t *q2, const float *scale2,
                            const uint8_t *zero2, samd_fmt wf, int32_t group, int64_t T, int64_t M, int64_t K,
