@@ -152,12 +152,14 @@ __device__ __forceinline__ ZeroPoint zero_point(uint32_t z) {   // of 0 .. 255
     const half2_t k960 = {(half_t)960.0f, (half_t)960.0f};
     return {-at1024, k960 - at1024};
 }
+
 // -(1024 + z) and -(64 + z) in one word.
 template <bool SIGNED>
 __device__ __forceinline__ float zero_point_word(uint32_t z) {
     const ZeroPoint p = zero_point<SIGNED>(z);
     return __uint_as_float(__builtin_bit_cast(uint32_t, half2_t{p.less[0], p.less16[0]}));
 }
+
 // The fields as such, put under bits: 1024 + u in [0] and [2], 1024 + 16 u in [1] and [3].
 template <bool SIGNED>
 __device__ __forceinline__ void field_pairs(uint32_t w, half2_t (&out)[4]) {
@@ -169,6 +171,7 @@ __device__ __forceinline__ void field_pairs(uint32_t w, half2_t (&out)[4]) {
     out[2] = __builtin_bit_cast(half2_t, (v & 0x000f000fu) ^ one);
     out[3] = __builtin_bit_cast(half2_t, (v & 0x00f000f0u) ^ sixteen);
 }
+
 template <bool SIGNED>
 __device__ __forceinline__ void whole_pairs(uint32_t w, const ZeroPoint &z, half2_t (&out)[4]) {
     const half2_t sixteenth = {(half_t)0.0625f, (half_t)0.0625f};

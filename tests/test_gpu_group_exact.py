@@ -131,6 +131,29 @@ def test_wide_products_of_few_tokens(typ):
     product_is_the_formulas(typ, 5, 260, 8200)
 
 
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 5, 20, 600])
+def test_zero_points_beyond_the_fields(typ, T):
+    """Zero points are bytes: differences down to -255 are whole numbers too."""
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    M, K = 300, 421
+    x, xv = matrix(gen, T, K, typ)
+    dy, dyv = matrix(gen, T, M, typ)
+    for group in (32, 64, 128):
+        q = torch.randint(0, 16, (M, K), generator=gen, device=DEV)
+        zero = torch.randint(0, 256, (M, -(-K // group)), generator=gen, device=DEV).to(torch.uint8)
+        zero[:, 0] = torch.arange(M, device=DEV) % 256
+        w, values = from_fields(gen, q, group, zero)
+        want, size = xv @ values.t(), xv.abs() @ values.abs().t()
+        bound = rounding(typ, want) + (K / 32 + 64) * 2.0 ** -24 * size
+        off = ((samd.group_matmul(x, w).double() - want).abs() - bound).max().item()
+        assert off <= 0, (group, off)
+        want, size = dyv @ values, dyv.abs() @ values.abs()
+        bound = rounding(typ, want) + (LOST[typ] + (M / 32 + 64) * 2.0 ** -24) * size
+        off = ((samd.group_matmul_grad(dy, w).double() - want).abs() - bound).max().item()
+        assert off <= 0, ("dx", group, off)
+
+
 # What a product dy w may lose on its way into a gradient, as a part of it.  bf16: the weight rounded to a bf16, 2^-8.
 # f16: both cut to 8 bits, what is cut off below 2^-7 of each (of dy's 11 bits, at most 7/8 of that); the weight's cut-off
 # part is rounded to 8 bits, 2^-8 of at most 2^-8 where it is largest, 2^-16; the product of the cut-off parts is left out,
